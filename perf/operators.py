@@ -187,7 +187,7 @@ def _prepare_preference(c, seed, s):
     s["place"] = torch.arange(rows, device="cuda") - s["offsets"][s["seq"]]
     s["labels"][s["place"] < torch.tensor([p for _, p in lens], device="cuda")[s["seq"]]] = -100
     s["logps"] = torch.empty(len(lens), device="cuda")
-    s["work"] = torch.empty(2 * rows, device="cuda")
+    s["work"] = torch.empty(2 * rows + len(lens), device="cuda")
     if c["op"] == "preference":
         # the frozen reference model gives each sequence about what the policy does
         own_lp = torch.cat([_row_logps(s["logits"][a:a + 4096], s["labels"][a:a + 4096])[0] for a in range(0, rows, 4096)])
