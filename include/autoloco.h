@@ -472,6 +472,154 @@ int autoloco_last_adamw_ms(autoloco_ctx* ctx, float* norm_ms, float* update_ms);
 int autoloco_adamw_traffic_reference(autoloco_ctx* ctx, const autoloco_adamw_buffers* bufs);
 
 /* ------------------------------------------------------------------------ */
+/* Operators of a worker's local step                                        */
+/* ------------------------------------------------------------------------ */
+
+/* What comes before the optimiser in a local step of preference tuning: linear
+ * layers whose operands are held in microscaled 4-bit floating point, the
+ * preference loss over paired sequences with its gradient, and the global norm
+ * and clipping of each worker's gradient over its many tensors.  The buffers of
+ * these calls are matrices with a row stride, need no more alignment than their
+ * elements (4-bit codes: 16 bytes, scales: 4), and may have any size, also 0.
+ * An output may overlap nothing else the call is given, except where said. */
+
+/* rows x cols elements of dtype (autoloco_dtype), row r at data + r * stride
+ * elements.  stride >= cols for an output of more than one row; an input may
+ * have any stride >= 0 (0: the same row again and again).
+ * rows, cols in 0..2^30, stride in 0..2^40. */
+typedef struct {
+    void* data;
+    int64_t rows, cols, stride;
+    int32_t dtype;
+} autoloco_matrix;
+
+/* A matrix in microscaled 4-bit floating point: along each row, 32 columns share
+ * one scale 2^(s - 127) (s a byte; 255 means that all 32 values are NaN) and each
+ * value is that scale times one of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} (a code of 4 bits:
+ * sign, then two bits of exponent and one of mantissa).
+ *   codes:  [rows][64 * ceil(cols / 128)] bytes, two columns a byte, the even one in
+ *           the low half; 16-byte aligned.
+ *   scales: [ceil(cols / 128)][rows][4] bytes: the scales of the four blocks of 128
+ *           columns of one row are one word, and the words of neighbouring rows
+ *           are neighbours, as the matrix instructions take them; 4-byte aligned.
+ * Columns beyond cols in the last 128 have code 0 and, in blocks with no column at
+ * all, scale 127.  rows * ceil(cols / 128) < 2^31. */
+typedef struct {
+    int64_t rows, cols;
+    uint8_t* codes;
+    uint8_t* scales;
+} autoloco_mxfp4;
+
+/* Quantises x: into q (blocks along x's rows; q is rows x cols) and into qt
+ * (blocks along x's columns; qt is cols x rows, the transposed matrix), either of
+ * which may be NULL, from one reading of x.  A block's scale is 2^(floor(log2
+ * max|x|) - 2), at least 2^-127 (a block of zeros: 1); each value divided by it
+ * is rounded to the nearest representable one, ties to the even code, and
+ * anything above 6 becomes 6.  A block with an infinity or a NaN becomes 32 NaNs.
+ * Asynchronous on the stream.
+ * Errors: E_INVALID, E_ALIGN, E_ALIAS, E_DEVICE. */
+int autoloco_mxfp4_quantize(autoloco_ctx* ctx, const autoloco_matrix* x, const autoloco_mxfp4* q,
+                            const autoloco_mxfp4* qt);
+/* The values q stands for, into out (exact in fp32 and in bf16).  Asynchronous.
+ * Errors: as above. */
+int autoloco_mxfp4_dequantize(autoloco_ctx* ctx, const autoloco_mxfp4* q, const autoloco_matrix* out);
+/* out[m][n] = sum_k a[m][k] b[n][k]: the product of a with the transpose of b, both
+ * with blocks along the summed axis, accumulated in fp32 in a fixed order and
+ * rounded once.  A linear layer's forward pass is a = x, b = W ([out][in]); its
+ * gradients are dx: a = dy, b = W's qt form, and dW: a = dy's qt, b = x's qt form.
+ * a and b may be the same.  With cols = 0 out is zero.  Asynchronous.
+ * Errors: as above (E_INVALID: shapes that do not fit). */
+int autoloco_mxfp4_matmul(autoloco_ctx* ctx, const autoloco_mxfp4* a, const autoloco_mxfp4* b,
+                          const autoloco_matrix* out);
+/* y = x W^T with x quantised on the way (the values are those of quantize and
+ * matmul).  Up to AUTOLOCO_MXFP4_TOKENS rows (tokens being decoded) x is quantised
+ * inside the product and xq is not used (may be NULL); beyond, xq (x's shape)
+ * receives x's 4-bit form.  Asynchronous.  Errors: as above. */
+#define AUTOLOCO_MXFP4_TOKENS 16
+int autoloco_mxfp4_linear(autoloco_ctx* ctx, const autoloco_matrix* x, const autoloco_mxfp4* w,
+                          const autoloco_matrix* y, const autoloco_mxfp4* xq);
+
+/* A batch of token sequences and the logits a model gives them: row r of logits
+ * scores labels[r], the token at (or after, as the caller aligns them) row r.
+ *   logits:    [rows][vocab], fp32 or bf16.
+ *   labels:    [rows] int64 in device memory; a label outside 0..vocab-1 masks its
+ *              row: the row adds nothing and is not read.
+ *   offsets:   [sequences + 1] int64 in device memory: sequence s is rows
+ *              offsets[s]..offsets[s+1]-1; non-decreasing.  Values outside 0..rows
+ *              count as the nearer end.  Sequences may be empty; rows of no
+ *              sequence are masked.
+ *   work:      [2 * rows + sequences] fp32, written: each row's log sum exp and its
+ *              label's log-probability (both 0 where masked), then each sequence's
+ *              weight in the gradient (autoloco_preference_loss). */
+typedef struct {
+    autoloco_matrix logits;
+    const int64_t* labels;
+    const int64_t* offsets;
+    int64_t sequences;   /* 0..2^20 */
+    float* work;
+} autoloco_sequences;
+
+/* logps[s] = sum over the rows of sequence s of log softmax(logits[r])[labels[r]]
+ * ([sequences] fp32, summed in fp64 in a fixed order): what the frozen reference model
+ * gives each sequence.  Asynchronous.
+ * Errors: E_INVALID, E_ALIGN, E_ALIAS, E_DEVICE. */
+int autoloco_sequence_logps(autoloco_ctx* ctx, const autoloco_sequences* s, float* logps);
+
+/* The preference loss of pairs of sequences, the chosen ones first (0..P-1), then
+ * the rejected ones in the same order (P..2P-1; sequences = 2P):
+ *   z_p = beta ((logp_p - ref_p) - (logp_{P+p} - ref_{P+p}))
+ *   loss_p = -(1 - smoothing) log sigma(z_p) - smoothing log sigma(-z_p)
+ * and the gradient of grad_scale * sum_p loss_p by the logits,
+ *   grads[r][v] = w_s ([v = labels[r]] - softmax(logits[r])[v]),
+ *   w_p = grad_scale beta (sigma(z_p) - (1 - smoothing)), w_{P+p} = -w_p,
+ * zero in masked rows whatever their logits hold.  Logits of -inf have probability
+ * 0; a row with a NaN or +inf, or nothing but -inf, makes its pair NaN.
+ *   ref_logps: [2P] fp32;  losses: [P] fp32;  logps: [2P] fp32;
+ *   grads: NULL data (no gradient), or the logits' shape and dtype; may be the
+ *   logits themselves (same data, same stride), which it then overwrites.
+ * smoothing in [0, 1], beta and grad_scale finite.  Asynchronous.
+ * Errors: E_INVALID, E_ALIGN, E_ALIAS, E_DEVICE. */
+typedef struct {
+    const float* ref_logps;
+    float* losses;
+    float* logps;
+    autoloco_matrix grads;
+    double beta, smoothing, grad_scale;
+} autoloco_preference;
+int autoloco_preference_loss(autoloco_ctx* ctx, const autoloco_sequences* s, const autoloco_preference* p);
+
+/* One tensor of a worker's gradient: n contiguous elements (0..2^40).  packed: [n]
+ * fp32 that receives the clipped gradient, or NULL: grad itself is clipped in place
+ * (bf16: rounded to nearest even). */
+typedef struct {
+    void* grad;
+    float* packed;
+    int64_t n;
+    int32_t dtype;
+    int32_t worker;
+} autoloco_grad;
+/* A list of gradient tensors of `workers` (1..AUTOLOCO_MAX_K) workers, laid out once
+ * for the steps to come: the table of their places is copied to the device, the
+ * tensors stay the caller's and have to stay where they are until the list is
+ * destroyed.  All have a packed place or none.  0 <= count <= 2^20.
+ * Errors: E_INVALID, E_ALIGN, E_ALIAS (two tensors overlap), E_DEVICE, E_NOMEM. */
+typedef struct autoloco_grads autoloco_grads;
+int autoloco_grads_create(autoloco_ctx* ctx, const autoloco_grad* tensors, int64_t count, int32_t workers,
+                          autoloco_grads** out);
+/* Waits for the device's work and frees the list (NULL is a no-op). */
+void autoloco_grads_destroy(autoloco_grads* list);
+/* Each worker's gradient norm over all its tensors, ||g||, and c = min(1, max_norm
+ * / (||g|| + 1e-6)) as in autoloco_inner_adamw (max_norm = 0: c = 1): packed (or
+ * grad) becomes c g.  Squares are summed in fp64 in a fixed order.  norms: [workers]
+ * fp32 in device memory, or NULL.  With out the call blocks until the norms are on
+ * the host; without, it is asynchronous.  A non-finite gradient propagates
+ * (finite = 0).  Feed the packed gradients to autoloco_inner_adamw with
+ * max_grad_norm = 0.
+ * Errors: E_INVALID (also a context of another device), E_ALIGN, E_ALIAS, E_DEVICE. */
+int autoloco_clip_grad_norm(autoloco_ctx* ctx, autoloco_grads* list, double max_norm, float* norms,
+                            autoloco_adamw_stats* out);
+
+/* ------------------------------------------------------------------------ */
 /* Host-only scalar routines                                                 */
 /* ------------------------------------------------------------------------ */
 

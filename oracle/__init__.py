@@ -31,6 +31,9 @@ Modules
                 pseudo-gradients (the payload of the paper's main runs).
   adamw       — one inner AdamW step of every worker with its own
                 gradient-norm clipping (Table "Training settings"; App. G.1).
+  mxfp4       — microscaled 4-bit floating point: quantisation, values, layout.
+  preference  — the preference loss over pairs of sequences with its gradient,
+                and clipping over many tensors.
 
 Parity unpinned (no value printed by the paper and no closed form fixes them;
 each is one reading of a point the paper leaves open):

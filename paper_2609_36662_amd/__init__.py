@@ -5,7 +5,10 @@ Nesterov outer step and the replica reset), and the workers' inner AdamW
 step between rounds, run in hand-written HIP kernels
 behind the C ABI of include/autoloco.h; the interval controller and the outer
 correction are host C++ behind the same ABI.  This package is the thin Python
-binding (same names as the C calls) and the in-tree build.
+binding (same names as the C calls) and the in-tree build.  What precedes the
+optimiser in a local step of preference tuning is here too: linear layers with
+microscaled 4-bit operands, the preference loss with its gradient, and clipping
+over many gradient tensors.
 """
 from ._lib import (  # noqa: F401
     BF16, F32, FUSE_RESET, FUSE_STATS, MAX_K, AutolocoError, Context, Controller,
@@ -18,4 +21,7 @@ from ._lib import (  # noqa: F401
     autoloco_inner_adamw, autoloco_last_adamw_ms, autoloco_adamw_traffic_reference, autoloco_rank_payload, autoloco_shard_step, make_adamw_buffers, make_adamw_coeffs,
     autoloco_traffic_reference, autoloco_traffic_probe, autoloco_build_id, autoloco_outer_step_static,
     PROBE_READ, PROBE_WRITE, PROBE_RUN1, PROBE_RUN2, PROBE_SERIAL, PROBE_TILE, PROBE_PHASED, PROBE_RUN8,
+    GradList, Mxfp4, autoloco_clip_grad_norm, autoloco_grads_create, autoloco_grads_destroy,
+    autoloco_mxfp4_dequantize, autoloco_mxfp4_linear, autoloco_mxfp4_matmul, autoloco_mxfp4_quantize,
+    autoloco_preference_loss, autoloco_sequence_logps, make_matrix, make_sequences,
 )

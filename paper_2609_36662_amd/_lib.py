@@ -119,6 +119,30 @@ class AdamWStats(C.Structure):
                 ("k", C.c_int32), ("finite", C.c_int32)]
 
 
+class Matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("stride", C.c_int64),
+                ("dtype", C.c_int32)]
+
+
+class Mxfp4Buffers(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class Sequences(C.Structure):
+    _fields_ = [("logits", Matrix), ("labels", C.c_void_p), ("offsets", C.c_void_p), ("sequences", C.c_int64),
+                ("work", C.c_void_p)]
+
+
+class Preference(C.Structure):
+    _fields_ = [("ref_logps", C.c_void_p), ("losses", C.c_void_p), ("logps", C.c_void_p), ("grads", Matrix),
+                ("beta", C.c_double), ("smoothing", C.c_double), ("grad_scale", C.c_double)]
+
+
+class Grad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("packed", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32),
+                ("worker", C.c_int32)]
+
+
 # ---------------------------------------------------------------- loading --
 _lib = None
 _lock = threading.Lock()
@@ -159,6 +183,18 @@ SYMBOLS = [
                                        C.POINTER(AdamWStats)]),
     ("autoloco_last_adamw_ms", C.c_int, [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_float)]),
     ("autoloco_adamw_traffic_reference", C.c_int, [C.c_void_p, C.POINTER(AdamWBuffers)]),
+    ("autoloco_mxfp4_quantize", C.c_int, [C.c_void_p, C.POINTER(Matrix), C.POINTER(Mxfp4Buffers),
+                                          C.POINTER(Mxfp4Buffers)]),
+    ("autoloco_mxfp4_dequantize", C.c_int, [C.c_void_p, C.POINTER(Mxfp4Buffers), C.POINTER(Matrix)]),
+    ("autoloco_mxfp4_matmul", C.c_int, [C.c_void_p, C.POINTER(Mxfp4Buffers), C.POINTER(Mxfp4Buffers),
+                                        C.POINTER(Matrix)]),
+    ("autoloco_mxfp4_linear", C.c_int, [C.c_void_p, C.POINTER(Matrix), C.POINTER(Mxfp4Buffers), C.POINTER(Matrix),
+                                        C.POINTER(Mxfp4Buffers)]),
+    ("autoloco_sequence_logps", C.c_int, [C.c_void_p, C.POINTER(Sequences), C.c_void_p]),
+    ("autoloco_preference_loss", C.c_int, [C.c_void_p, C.POINTER(Sequences), C.POINTER(Preference)]),
+    ("autoloco_grads_create", C.c_int, [C.c_void_p, C.POINTER(Grad), C.c_int64, C.c_int32, C.POINTER(C.c_void_p)]),
+    ("autoloco_grads_destroy", None, [C.c_void_p]),
+    ("autoloco_clip_grad_norm", C.c_int, [C.c_void_p, C.c_void_p, C.c_double, C.c_void_p, C.POINTER(AdamWStats)]),
     ("autoloco_inner_lr", C.c_double, [C.POINTER(Schedule), C.c_int64]),
     ("autoloco_lr_mass", C.c_double, [C.POINTER(Schedule), C.c_int64, C.c_int64]),
     ("autoloco_outer_correction", C.c_int, [C.POINTER(OuterCfg), C.c_double, C.c_double,
@@ -657,6 +693,174 @@ def autoloco_last_adamw_ms(ctx: Context):
     a, b = C.c_float(), C.c_float()
     _check(lib().autoloco_last_adamw_ms(ctx.handle, C.byref(a), C.byref(b)), "autoloco_last_adamw_ms", ctx)
     return a.value, b.value
+
+
+# ------------------------------------------- operators of a worker's local step --
+def make_matrix(t, what: str = "matrix") -> Matrix:
+    """Describe a two-dimensional device tensor whose rows are contiguous (no copies)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        raise TypeError(f"{what} must be a two-dimensional CUDA (HIP) tensor")
+    dtype = t.dtype
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise TypeError(f"{what} must be float32 or bfloat16, got {dtype}")
+    rows, cols = t.shape
+    stride, inner = t.stride()
+    if inner != 1 and cols > 1 and rows > 0:
+        raise ValueError(f"the rows of {what} must be contiguous")
+    return Matrix(t.data_ptr(), rows, cols, stride, F32 if dtype is torch.float32 else BF16)
+
+
+class Mxfp4:
+    """A rows x cols matrix in microscaled 4-bit floating point, in caller-owned
+    device tensors: codes (uint8, rows x 64 ceil(cols / 128) bytes) and scales
+    (uint8, ceil(cols / 128) x rows x 4 bytes)."""
+
+    def __init__(self, rows: int, cols: int, codes, scales):
+        import torch
+        groups = (cols + 127) // 128
+        for t, n, what in ((codes, rows * groups * 64, "codes"), (scales, rows * groups * 4, "scales")):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.uint8 or not t.is_contiguous():
+                raise TypeError(f"{what} must be a contiguous CUDA (HIP) uint8 tensor")
+            if t.numel() != n:
+                raise ValueError(f"{what} of {rows} x {cols} takes {n} bytes, got {t.numel()}")
+        self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
+        self.buffers = Mxfp4Buffers(rows, cols, codes.data_ptr(), scales.data_ptr())
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda") -> "Mxfp4":
+        """Room for a rows x cols matrix."""
+        import torch
+        groups = (cols + 127) // 128
+        return cls(rows, cols, torch.empty((rows, 64 * groups), dtype=torch.uint8, device=device),
+                   torch.empty((groups, rows, 4), dtype=torch.uint8, device=device))
+
+
+def _mx(q):
+    return C.byref(q.buffers) if q is not None else None
+
+
+def autoloco_mxfp4_quantize(ctx: Context, x, q: Optional[Mxfp4] = None, qt: Optional[Mxfp4] = None) -> None:
+    """x's 4-bit form with blocks along its rows into q, along its columns (transposed) into qt."""
+    m = make_matrix(x, "x")
+    _check(lib().autoloco_mxfp4_quantize(ctx.handle, C.byref(m), _mx(q), _mx(qt)), "autoloco_mxfp4_quantize", ctx)
+
+
+def autoloco_mxfp4_dequantize(ctx: Context, q: Mxfp4, out) -> None:
+    """The values q stands for, into out."""
+    m = make_matrix(out, "out")
+    _check(lib().autoloco_mxfp4_dequantize(ctx.handle, _mx(q), C.byref(m)), "autoloco_mxfp4_dequantize", ctx)
+
+
+def autoloco_mxfp4_matmul(ctx: Context, a: Mxfp4, b: Mxfp4, out) -> None:
+    """out = a b^T."""
+    m = make_matrix(out, "out")
+    _check(lib().autoloco_mxfp4_matmul(ctx.handle, _mx(a), _mx(b), C.byref(m)), "autoloco_mxfp4_matmul", ctx)
+
+
+def autoloco_mxfp4_linear(ctx: Context, x, w: Mxfp4, y, xq: Optional[Mxfp4] = None) -> None:
+    """y = x w^T with x quantised on the way; xq (x's shape) holds its 4-bit form when x has more than 16 rows."""
+    mx, my = make_matrix(x, "x"), make_matrix(y, "y")
+    _check(lib().autoloco_mxfp4_linear(ctx.handle, C.byref(mx), _mx(w), C.byref(my), _mx(xq)),
+           "autoloco_mxfp4_linear", ctx)
+
+
+def make_sequences(logits, labels, offsets, work) -> Sequences:
+    """Describe a batch of token sequences: logits [rows, vocab], labels [rows] and
+    offsets [sequences + 1] int64, work at least 2 rows + sequences float32."""
+    import torch
+    m = make_matrix(logits, "logits")
+    rows, count = m.rows, offsets.numel() - 1
+    for t, dtype, n, what in ((labels, torch.int64, rows, "labels"), (offsets, torch.int64, 1, "offsets"),
+                              (work, torch.float32, 2 * rows + count, "work")):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype or not t.is_contiguous():
+            raise TypeError(f"{what} must be a contiguous CUDA (HIP) {dtype} tensor")
+        if t.numel() < n:
+            raise ValueError(f"{what} is shorter than {n}")
+    return Sequences(m, labels.data_ptr(), offsets.data_ptr(), count, work.data_ptr())
+
+
+def autoloco_sequence_logps(ctx: Context, logits, labels, offsets, logps, work) -> None:
+    """Each sequence's log-probability under the logits, into logps [sequences] float32."""
+    import torch
+    s = make_sequences(logits, labels, offsets, work)
+    _check(lib().autoloco_sequence_logps(ctx.handle, C.byref(s), _cuda_contig(logps, torch.float32, s.sequences, "logps")),
+           "autoloco_sequence_logps", ctx)
+
+
+def autoloco_preference_loss(ctx: Context, logits, labels, offsets, ref_logps, losses, logps, work, grads=None,
+                             beta: float = 0.1, label_smoothing: float = 0.0, grad_scale: float = 1.0) -> None:
+    """The preference loss of each pair (the chosen sequences first, then the rejected
+    ones in the same order) into losses, the sequences' log-probabilities into logps and,
+    with grads, the gradient of grad_scale times the losses' sum by the logits; grads may be logits."""
+    import torch
+    s = make_sequences(logits, labels, offsets, work)
+    f32, n = torch.float32, s.sequences
+    p = Preference(_cuda_contig(ref_logps, f32, n, "ref_logps"), _cuda_contig(losses, f32, n // 2, "losses"),
+                   _cuda_contig(logps, f32, n, "logps"), make_matrix(grads, "grads") if grads is not None else Matrix(),
+                   beta, label_smoothing, grad_scale)
+    _check(lib().autoloco_preference_loss(ctx.handle, C.byref(s), C.byref(p)), "autoloco_preference_loss", ctx)
+
+
+class GradList:
+    """An autoloco_grads: the workers' gradient tensors, laid out once.  Holds them."""
+
+    def __init__(self, handle, workers: int, tensors):
+        self.handle, self.workers, self.tensors = handle, workers, tensors
+
+    def close(self):
+        h, self.handle = getattr(self, "handle", None), None
+        if h:
+            lib().autoloco_grads_destroy(h)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def autoloco_grads_create(ctx: Context, grads: Sequence[Sequence], packed: Optional[Sequence] = None) -> GradList:
+    """A list of each worker's gradient tensors (float32 or bfloat16, any shapes).  With packed, one flat float32
+    tensor a worker, the clipped gradients go there, one tensor after another; without, they are clipped in place."""
+    import torch
+    if not 1 <= len(grads) <= MAX_K:
+        raise ValueError(f"need 1..{MAX_K} workers, got {len(grads)}")
+    if packed is not None and len(packed) != len(grads):
+        raise ValueError("one packed tensor per worker")
+    flat = []
+    for k, worker in enumerate(grads):
+        at = 0
+        for t in worker:
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+                raise TypeError("gradients must be contiguous CUDA (HIP) tensors")
+            n = t.numel()
+            flat.append((t.data_ptr(), at, n, _dtype_code(t), k))
+            at += n
+        if packed is not None:
+            _cuda_contig(packed[k], torch.float32, at, "packed")
+    arr = (Grad * max(1, len(flat)))()
+    for i, (ptr, at, n, code, k) in enumerate(flat):
+        arr[i] = Grad(ptr, packed[k].data_ptr() + 4 * at if packed is not None else None, n, code, k)
+    h = C.c_void_p()
+    _check(lib().autoloco_grads_create(ctx.handle, arr, len(flat), len(grads), C.byref(h)), "autoloco_grads_create", ctx)
+    return GradList(h, len(grads), ([list(w) for w in grads], list(packed) if packed is not None else None))
+
+
+def autoloco_grads_destroy(grads: GradList) -> None:
+    grads.close()
+
+
+def autoloco_clip_grad_norm(ctx: Context, grads: GradList, max_norm: float, norms=None,
+                            stats: bool = True) -> Optional[AdamWStats]:
+    """Clips every worker's gradient to max_norm (0: not at all); norms, a float32 device tensor, receives the workers'
+    norms.  Returns them and the coefficients (stats=True) or None (asynchronous on the context's stream)."""
+    import torch
+    out = AdamWStats() if stats else None
+    _check(lib().autoloco_clip_grad_norm(ctx.handle, grads.handle, float(max_norm),
+                                         _cuda_contig(norms, torch.float32, grads.workers, "norms") if norms is not None else None,
+                                         C.byref(out) if out is not None else None), "autoloco_clip_grad_norm", ctx)
+    return out
 
 
 def make_schedule(peak=4e-4, min_lr=0.0, warmup=1000, total=50_000) -> Schedule:

@@ -88,6 +88,8 @@ def jobs():
     cmds.append([hipcc, *HIP_FLAGS, "-c", os.path.join(CSRC, "shard_inst.hip"), "-o", os.path.join(BUILD, "shard.o")])
     cmds.append([hipcc, *HIP_FLAGS, "-c", os.path.join(CSRC, "reduce_inst.hip"), "-o", os.path.join(BUILD, "reduce.o")])
     cmds.append([hipcc, *HIP_FLAGS, "-c", os.path.join(CSRC, "probe_inst.hip"), "-o", os.path.join(BUILD, "probe.o")])
+    for name in ("mxfp4_inst", "preference_inst", "clip_inst", "local_api"):
+        cmds.append([hipcc, *HIP_FLAGS, "-c", os.path.join(CSRC, name + ".hip"), "-o", os.path.join(BUILD, name + ".o")])
     cmds.append([hipcc, *HIP_FLAGS, f'-DAUTOLOCO_BUILD_ID="{source_hash()}"', "-c", os.path.join(CSRC, "api.hip"),
                  "-o", os.path.join(BUILD, "api.o")])
     for src in ("scalar.cpp", "controller.cpp"):

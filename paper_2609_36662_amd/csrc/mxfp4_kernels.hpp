@@ -1,0 +1,313 @@
+// Microscaled 4-bit floating point on gfx950: quantisation along the rows and the
+// columns of a matrix, the values back, and products.
+//
+// A block of 32 values x shares the scale 2^e, e = floor(log2 max|x|) - 2: the
+// largest magnitude lands in [4, 8) of the representable {0, .5, 1, 1.5, 2, 3, 4, 6}.
+// The exponent field of max|x| gives e + 129 directly.  The conversion instructions
+// divide by the scale, round to nearest even and saturate at 6.  The matrix
+// instructions take the codes and scales as they are stored, 32 values a lane, and
+// add the products up in fp32.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "matrix_view.hpp"
+
+namespace autoloco {
+
+struct Mx4 {
+    uint8_t* codes;
+    uint8_t* scales;
+    int64_t rows;
+    int64_t row_bytes;   // 64 * groups
+    int32_t groups;      // ceil(cols / 128)
+};
+
+typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr uint32_t kScaleOne = 127, kScaleNan = 255;
+
+// The scale byte of a block from the bits of its largest magnitude (an infinity or
+// a NaN has the largest bits of all).
+__device__ __forceinline__ uint32_t mx_scale(uint32_t amax_bits) {
+    const uint32_t e = amax_bits >> 23;
+    return amax_bits == 0 ? kScaleOne : e == 255 ? kScaleNan : e > 2 ? e - 2 : 0;
+}
+
+// Codes of 8 values under scale byte s, the first in the lowest bits.
+__device__ __forceinline__ uint32_t mx_codes8(const float (&x)[8], uint32_t s) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[i];
+    if (s < 32) {   // scales below the normal range of the instruction's fp32 operand
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] *= 0x1p32f;
+        s += 32;
+    }
+    if (s == kScaleNan) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = 0.f;
+        s = kScaleOne;
+    }
+    const float scale = __uint_as_float(s << 23);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], scale, 3);
+    return w;
+}
+
+// The values of 8 codes under scale byte s.
+__device__ __forceinline__ void mx_values8(float (&x)[8], uint32_t w, uint32_t s) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t c = w >> (4 * i) & 15u, m = c & 7u;
+        // magnitude: subnormal 0 and 0.5, else (1 + bit / 2) 2^(exponent - 1)
+        const float a = m < 2 ? 0.5f * (float)m : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
+        const float v = __builtin_ldexpf(a, (int)s - 127);
+        x[i] = s == kScaleNan ? __uint_as_float(0x7FC00000u) : c & 8u ? -v : v;
+    }
+}
+
+__device__ __forceinline__ uint32_t max_bits(float x, uint32_t m) {
+    const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
+    return b > m ? b : m;
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+    return o > v ? o : v;
+}
+
+// ---------------------------------------------------------------- quantise --
+// Along the rows: a lane takes 8 columns, four lanes a block.  Bound by reading x.
+template <bool BF16>
+__global__ void __launch_bounds__(kBlock) mx_rows_kernel(MatrixView x, Mx4 q) {
+    const int64_t t = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    const uint32_t unit = (uint32_t)(t >> 4);   // 128 columns of a row
+    const uint32_t row = unit / (uint32_t)q.groups, group = unit % (uint32_t)q.groups;
+    if (row >= q.rows) return;
+    const int piece = t & 15;
+    const int64_t col = (int64_t)group * 128 + piece * 8;
+    const char* src = static_cast<const char*>(x.data) + (int64_t)row * x.stride * (BF16 ? 2 : 4);
+    float v[8];
+    load8<BF16>(v, src, col, x.cols);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max_bits(v[i], m);
+    m = max_dpp<0xB1>(m);   // lanes ^ 1, then ^ 2: the block's four
+    m = max_dpp<0x4E>(m);
+    const uint32_t s = mx_scale(m);
+    *reinterpret_cast<uint32_t*>(q.codes + (int64_t)row * q.row_bytes + group * 64 + piece * 4) = mx_codes8(v, s);
+    if ((piece & 3) == 0) q.scales[((int64_t)group * q.rows + row) * 4 + (piece >> 2)] = (uint8_t)s;
+}
+
+// Along the columns (and the rows): a workgroup takes 128 rows of 256 bytes into
+// LDS, where a lane then reads 32 rows of one word: one fp32 column or two bf16 ones.
+template <bool BF16, bool ROWS>
+__global__ void __launch_bounds__(kBlock) mx_cols_kernel(MatrixView x, Mx4 q, Mx4 qt, uint32_t tiles) {
+    constexpr int E = BF16 ? 2 : 1;          // elements a word
+    constexpr int W = 64 * E;                // columns of a tile
+    __shared__ uint32_t tile[128 * 64];
+    const uint32_t rt = blockIdx.x / tiles, ct = blockIdx.x % tiles;
+    const int64_t r0 = (int64_t)rt * 128, c0 = (int64_t)ct * W;
+    const int lane16 = threadIdx.x & 15;
+    for (int p = 0; p < 8; ++p) {
+        const int r = p * 16 + (threadIdx.x >> 4);
+        const int64_t row = r0 + r;
+        const char* src = static_cast<const char*>(x.data) + row * x.stride * (BF16 ? 2 : 4);
+        const int64_t c = c0 + lane16 * 4 * E;
+        u32x4 w = {0, 0, 0, 0};
+        if (row < x.rows) {
+            if (c + 4 * E <= x.cols) {
+                w = *reinterpret_cast<const u32x4_any*>(src + c * (BF16 ? 2 : 4));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4 * E; ++i)
+                    if (c + i < x.cols) {
+                        if constexpr (BF16)
+                            w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(src)[c + i] << (16 * (i & 1));
+                        else
+                            w[i] = reinterpret_cast<const uint32_t*>(src)[c + i];
+                    }
+            }
+        }
+        *reinterpret_cast<u32x4*>(&tile[r * 64 + lane16 * 4]) = w;
+        if constexpr (ROWS) {
+            float v[8] = {};
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (BF16) {
+                    v[2 * j] = bf16_lo(w[j]);
+                    v[2 * j + 1] = bf16_hi(w[j]);
+                } else {
+                    v[j] = __uint_as_float(w[j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4 * E; ++j) m = max_bits(v[j], m);
+            m = max_dpp<0xB1>(m);
+            m = max_dpp<0x4E>(m);
+            if constexpr (!BF16) m = max_dpp<0x141>(m);   // 7 - lane inside each 8: the other four of the block
+            const uint32_t s = mx_scale(m), code = mx_codes8(v, s);
+            const int64_t group = c0 / 128;
+            if (row < x.rows) {
+                uint8_t* d = q.codes + row * q.row_bytes + c / 2;
+                if constexpr (BF16)
+                    *reinterpret_cast<uint32_t*>(d) = code;
+                else
+                    *reinterpret_cast<uint16_t*>(d) = (uint16_t)code;
+                if ((lane16 & (BF16 ? 3 : 7)) == 0)
+                    q.scales[(group * q.rows + row) * 4 + (c % 128) / 32] = (uint8_t)s;
+            }
+        }
+    }
+    __syncthreads();
+    const int word = threadIdx.x & 63, blk = threadIdx.x >> 6;
+    uint32_t w[32];
+#pragma unroll
+    for (int r = 0; r < 32; ++r) w[r] = tile[(blk * 32 + r) * 64 + word];
+    __syncthreads();
+    // codes of the tile's columns through LDS: [W][4] pieces of 16 bytes
+#pragma unroll
+    for (int h = 0; h < E; ++h) {
+        float v[8];
+        uint32_t m = 0;
+        auto value = [&](int r) -> float {
+            if constexpr (BF16)
+                return h == 0 ? bf16_lo(w[r]) : bf16_hi(w[r]);
+            else
+                return __uint_as_float(w[r]);
+        };
+#pragma unroll
+        for (int r = 0; r < 32; ++r) m = max_bits(value(r), m);
+        const uint32_t s = mx_scale(m);
+        u32x4 code;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = value(8 * j + i);
+            code[j] = mx_codes8(v, s);
+        }
+        const int col = word * E + h;
+        *reinterpret_cast<u32x4*>(&tile[col * 16 + blk * 4]) = code;
+        if (c0 + col < x.cols) qt.scales[((int64_t)rt * qt.rows + c0 + col) * 4 + blk] = (uint8_t)s;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < E; ++p) {
+        const int i = p * kBlock + threadIdx.x, col = i >> 2;
+        if (c0 + col < x.cols)
+            *reinterpret_cast<u32x4*>(qt.codes + (c0 + col) * qt.row_bytes + (int64_t)rt * 64 + (i & 3) * 16) =
+                *reinterpret_cast<const u32x4*>(&tile[i * 4]);
+    }
+}
+
+// -------------------------------------------------------------- dequantise --
+template <bool BF16>
+__global__ void __launch_bounds__(kBlock) mx_values_kernel(Mx4 q, MatrixOut out) {
+    const int64_t t = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    const uint32_t unit = (uint32_t)(t >> 4);
+    const uint32_t row = unit / (uint32_t)q.groups, group = unit % (uint32_t)q.groups;
+    if (row >= q.rows) return;
+    const int piece = t & 15;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(q.codes + (int64_t)row * q.row_bytes + group * 64 + piece * 4);
+    const uint32_t s = q.scales[((int64_t)group * q.rows + row) * 4 + (piece >> 2)];
+    float v[8];
+    mx_values8(v, w, s);
+    store8<BF16>(static_cast<char*>(out.data) + (int64_t)row * out.stride * (BF16 ? 2 : 4),
+                 (int64_t)group * 128 + piece * 8, out.cols, v);
+}
+
+// ----------------------------------------------------------------- product --
+__device__ __forceinline__ i32x8 operand(u32x4 w) { return i32x8{(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0}; }
+
+// A wave 32 x 32 of the result, operands straight from memory.  A lane of the
+// 32x32x64 instruction holds row lane % 32, columns 32 (lane / 32) on; the result has
+// column lane % 32 and rows 8 (i / 4) + 4 (lane / 32) + i % 4.
+template <bool BF16>
+__global__ void __launch_bounds__(kBlock) mx_matmul_kernel(Mx4 a, Mx4 b, MatrixOut out, uint32_t ntiles) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t m0 = (int64_t)(blockIdx.x / ntiles) * 64 + (wave >> 1) * 32;
+    const int64_t n0 = (int64_t)(blockIdx.x % ntiles) * 64 + (wave & 1) * 32;
+    const int r = lane & 31, h = lane >> 5;
+    const int64_t am = m0 + r < a.rows ? m0 + r : a.rows - 1, bn = n0 + r < b.rows ? n0 + r : b.rows - 1;
+    const uint8_t* ap = a.codes + am * a.row_bytes + h * 16;
+    const uint8_t* bp = b.codes + bn * b.row_bytes + h * 16;
+    f32x16 acc = {};
+    for (int g = 0; g < a.groups; ++g) {
+        const uint32_t sa = *reinterpret_cast<const uint32_t*>(a.scales + ((int64_t)g * a.rows + am) * 4) >> (8 * h);
+        const uint32_t sb = *reinterpret_cast<const uint32_t*>(b.scales + ((int64_t)g * b.rows + bn) * 4) >> (8 * h);
+        const i32x8 a0 = operand(*reinterpret_cast<const u32x4*>(ap + g * 64));
+        const i32x8 b0 = operand(*reinterpret_cast<const u32x4*>(bp + g * 64));
+        const i32x8 a1 = operand(*reinterpret_cast<const u32x4*>(ap + g * 64 + 32));
+        const i32x8 b1 = operand(*reinterpret_cast<const u32x4*>(bp + g * 64 + 32));
+        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a0, b0, acc, 4, 4, 0, (int)sa, 0, (int)sb);
+        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a1, b1, acc, 4, 4, 2, (int)sa, 2, (int)sb);
+    }
+    const int64_t n = n0 + r;
+    if (n >= out.cols) return;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int64_t m = m0 + 8 * (i / 4) + 4 * h + i % 4;
+        if (m < out.rows) store_one<BF16>(out.data, m * out.stride + n, acc[i]);
+    }
+}
+
+// Up to 16 rows of x, quantised as they are read.  A lane of the 16x16x128 instruction
+// holds row lane % 16, columns 32 (lane / 16) on: exactly one block, so its scale
+// needs no other lane.  A workgroup takes 16 rows of the weight, its four waves a
+// quarter of the columns each, joined in LDS.  Bound by reading the weight.
+template <bool BF16>
+__global__ void __launch_bounds__(kBlock) mx_tokens_kernel(MatrixView x, Mx4 w, MatrixOut y) {
+    __shared__ float part[4][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r = lane & 15, j = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t wn = n0 + r < w.rows ? n0 + r : w.rows - 1;
+    const int64_t xm = r < x.rows ? r : x.rows - 1;
+    const char* xr = static_cast<const char*>(x.data) + xm * x.stride * (BF16 ? 2 : 4);
+    f32x4 acc = {};
+    for (int g = wave; g < w.groups; g += 4) {
+        const u32x4 wc = *reinterpret_cast<const u32x4*>(w.codes + wn * w.row_bytes + (int64_t)g * 64 + j * 16);
+        const uint32_t ws = w.scales[((int64_t)g * w.rows + wn) * 4 + j];
+        float v[4][8];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            load8<BF16>(v[i], xr, (int64_t)g * 128 + j * 32 + i * 8, x.cols);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = max_bits(v[i][e], m);
+        }
+        const uint32_t s = mx_scale(m);
+        u32x4 xc;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xc[i] = mx_codes8(v[i], s);
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(wc), operand(xc), acc, 4, 4, 0, (int)ws, 0, (int)s);
+    }
+    *reinterpret_cast<f32x4*>(&part[wave][lane * 4]) = acc;
+    __syncthreads();
+    // thread t: token t / 16, row t % 16 of the weight
+    const int m = threadIdx.x >> 4, n = threadIdx.x & 15;
+    const int at = ((n >> 2) * 16 + m) * 4 + (n & 3);
+    const float sum = ((part[0][at] + part[1][at]) + part[2][at]) + part[3][at];
+    if (m < y.rows && n0 + n < y.cols) store_one<BF16>(y.data, m * y.stride + n0 + n, sum);
+}
+
+// Zeros where there is nothing to add up.
+template <bool BF16>
+__global__ void __launch_bounds__(kBlock) zero_matrix_kernel(MatrixOut out) {
+    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (i < out.rows * out.cols) store_one<BF16>(out.data, i / out.cols * out.stride + i % out.cols, 0.f);
+}
+
+hipError_t launch_mx_quantize(bool bf16, const MatrixView& x, const Mx4* q, const Mx4* qt, hipStream_t s);
+hipError_t launch_mx_values(bool bf16, const Mx4& q, const MatrixOut& out, hipStream_t s);
+hipError_t launch_mx_matmul(bool bf16, const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t s);
+hipError_t launch_mx_tokens(bool bf16, const MatrixView& x, const Mx4& w, const MatrixOut& y, hipStream_t s);
+
+}  // namespace autoloco
