@@ -527,7 +527,7 @@ int autoloco_mxfp4_dequantize(autoloco_ctx* ctx, const autoloco_mxfp4* q, const 
  * with blocks along the summed axis, accumulated in fp32 in a fixed order and
  * rounded once.  A linear layer's forward pass is a = x, b = W ([out][in]); its
  * gradients are dx: a = dy, b = W's qt form, and dW: a = dy's qt, b = x's qt form.
- * a and b may be the same.  With cols = 0 out is zero.  Asynchronous.
+ * a and b may be the same.  At most 2^24 columns; with none, out is zero.  Asynchronous.
  * Errors: as above (E_INVALID: shapes that do not fit). */
 int autoloco_mxfp4_matmul(autoloco_ctx* ctx, const autoloco_mxfp4* a, const autoloco_mxfp4* b,
                           const autoloco_matrix* out);

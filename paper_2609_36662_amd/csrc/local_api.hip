@@ -23,6 +23,9 @@ namespace {
 constexpr int64_t kMaxDim = int64_t(1) << 30;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
+// Columns of a product: a tile's rows lie within 32 bits of its first.
+constexpr int64_t kMaxProductCols = int64_t(1) << 24;
+
 // Runs a call's body: memory that runs out on the host is an error like any other.
 template <typename Body>
 int guarded(autoloco_ctx* c, Body body) {
@@ -209,6 +212,7 @@ int autoloco_mxfp4_matmul(autoloco_ctx* c, const autoloco_mxfp4* a, const autolo
             return st;
         if (a->cols != w->cols || out->rows != a->rows || out->cols != w->rows)
             return fail(c, AUTOLOCO_E_INVALID, "shapes do not fit: out[m][n] = sum_k a[m][k] b[n][k]");
+        if (a->cols > kMaxProductCols) return fail(c, AUTOLOCO_E_INVALID, "more than 2^24 columns");
         Buffers b{c};
         add_mx(b, *a, "codes of a", "scales of a", false);
         add_mx(b, *w, "codes of b", "scales of b", false);
@@ -229,6 +233,7 @@ int autoloco_mxfp4_linear(autoloco_ctx* c, const autoloco_matrix* x, const autol
             return st;
         if (x->cols != w->cols || y->rows != x->rows || y->cols != w->rows)
             return fail(c, AUTOLOCO_E_INVALID, "shapes do not fit: y[m][n] = sum_k x[m][k] w[n][k]");
+        if (x->cols > kMaxProductCols) return fail(c, AUTOLOCO_E_INVALID, "more than 2^24 columns");
         if (x->dtype != y->dtype) return fail(c, AUTOLOCO_E_INVALID, "x and y have different dtypes");
         const bool tokens = x->rows <= AUTOLOCO_MXFP4_TOKENS;
         Buffers b{c};

@@ -1,5 +1,5 @@
 // Launchers of the 4-bit kernels.
-#include "mxfp4_kernels.hpp"
+#include "mxfp4_tiles.hpp"
 
 namespace autoloco {
 
@@ -24,16 +24,44 @@ hipError_t quantize(const MatrixView& x, const Mx4* q, const Mx4* qt, hipStream_
     return hipGetLastError();
 }
 
+// Which tile a product takes: 256 x 256 (one workgroup a compute unit, the most products
+// for every byte read from LDS), 128 x 128 (two) or 64 x 64.  From the times of full and
+// begun rounds of the chip's 256 compute units, in microseconds for g groups of 128
+// columns.  Measured (256, 128 and 64): 4,096 x 4,096 x 4,096 40, 45 and 66 us; 4,096 x
+// 11,008 x 4,096 106, 120 and 179; 4,608 x 4,096 x 4,096 (a second round barely begun) 62,
+// 56 and 74; 2,304 x 4,096 x 4,096 32, 35 and 40; 1,003 x 50,257 x 768 61, 43 and 55;
+// 1,024 x 4,096 x 2,048 18.1, 8.8 and 10.9; 512 x 4,096 x 2,048 17.7, 8.0 and 7.2.
+enum Tile { TILE_256, TILE_128, TILE_64 };
+Tile tile_for(int64_t m, int64_t n, int32_t groups) {
+    auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+    const double g = groups;
+    const int64_t t256 = tiles(256), t128 = tiles(128);
+    if (t128 < 176) return TILE_64;
+    const int64_t full256 = t256 / 256, rest256 = t256 % 256, full128 = t128 / 512, rest128 = t128 % 512;
+    const double us256 = full256 * (0.94 * g + 9.0) + (rest256 > 0 ? 0.75 * g + 8.0 : 0.0);
+    const double us128 = full128 * (0.62 * g + 2.5) + (rest128 > 256 ? 0.5 * g + 2.5 : rest128 > 0 ? 0.3 * g + 2.0 : 0.0);
+    return us256 < us128 ? TILE_256 : TILE_128;
+}
+
+template <int T, bool BF16>
+hipError_t tiles(const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t s) {
+    const TileGrid g{(uint32_t)((out.rows + 64 * T - 1) / (64 * T)), (uint32_t)((out.cols + 64 * T - 1) / (64 * T))};
+    hipLaunchKernelGGL((mx_tile_kernel<T, BF16>), dim3(g.mt * g.nt), dim3(256), 0, s, a, b, out, g);
+    return hipGetLastError();
+}
+
 template <bool BF16>
 hipError_t matmul(const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t s) {
     if (a.groups == 0) {
         const int64_t blocks = (out.rows * out.cols + kBlock - 1) / kBlock;
-        hipLaunchKernelGGL(zero_matrix_kernel<BF16>, dim3((unsigned)blocks), dim3(kBlock), 0, s, out);
+        hipLaunchKernelGGL(zero_matrix_kernel<BF16>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(kBlock), 0, s, out);
         return hipGetLastError();
     }
-    const uint32_t mt = (uint32_t)((out.rows + 63) / 64), nt = (uint32_t)((out.cols + 63) / 64);
-    hipLaunchKernelGGL(mx_matmul_kernel<BF16>, dim3(mt * nt), dim3(kBlock), 0, s, a, b, out, nt);
-    return hipGetLastError();
+    switch (tile_for(out.rows, out.cols, a.groups)) {
+        case TILE_256: return tiles<4, BF16>(a, b, out, s);
+        case TILE_128: return tiles<2, BF16>(a, b, out, s);
+        default: return tiles<1, BF16>(a, b, out, s);
+    }
 }
 
 }  // namespace

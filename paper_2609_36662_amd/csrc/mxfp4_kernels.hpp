@@ -226,38 +226,6 @@ __global__ void __launch_bounds__(kBlock) mx_values_kernel(Mx4 q, MatrixOut out)
 // ----------------------------------------------------------------- product --
 __device__ __forceinline__ i32x8 operand(u32x4 w) { return i32x8{(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0}; }
 
-// A wave 32 x 32 of the result, operands straight from memory.  A lane of the
-// 32x32x64 instruction holds row lane % 32, columns 32 (lane / 32) on; the result has
-// column lane % 32 and rows 8 (i / 4) + 4 (lane / 32) + i % 4.
-template <bool BF16>
-__global__ void __launch_bounds__(kBlock) mx_matmul_kernel(Mx4 a, Mx4 b, MatrixOut out, uint32_t ntiles) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t m0 = (int64_t)(blockIdx.x / ntiles) * 64 + (wave >> 1) * 32;
-    const int64_t n0 = (int64_t)(blockIdx.x % ntiles) * 64 + (wave & 1) * 32;
-    const int r = lane & 31, h = lane >> 5;
-    const int64_t am = m0 + r < a.rows ? m0 + r : a.rows - 1, bn = n0 + r < b.rows ? n0 + r : b.rows - 1;
-    const uint8_t* ap = a.codes + am * a.row_bytes + h * 16;
-    const uint8_t* bp = b.codes + bn * b.row_bytes + h * 16;
-    f32x16 acc = {};
-    for (int g = 0; g < a.groups; ++g) {
-        const uint32_t sa = *reinterpret_cast<const uint32_t*>(a.scales + ((int64_t)g * a.rows + am) * 4) >> (8 * h);
-        const uint32_t sb = *reinterpret_cast<const uint32_t*>(b.scales + ((int64_t)g * b.rows + bn) * 4) >> (8 * h);
-        const i32x8 a0 = operand(*reinterpret_cast<const u32x4*>(ap + g * 64));
-        const i32x8 b0 = operand(*reinterpret_cast<const u32x4*>(bp + g * 64));
-        const i32x8 a1 = operand(*reinterpret_cast<const u32x4*>(ap + g * 64 + 32));
-        const i32x8 b1 = operand(*reinterpret_cast<const u32x4*>(bp + g * 64 + 32));
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a0, b0, acc, 4, 4, 0, (int)sa, 0, (int)sb);
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a1, b1, acc, 4, 4, 2, (int)sa, 2, (int)sb);
-    }
-    const int64_t n = n0 + r;
-    if (n >= out.cols) return;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int64_t m = m0 + 8 * (i / 4) + 4 * h + i % 4;
-        if (m < out.rows) store_one<BF16>(out.data, m * out.stride + n, acc[i]);
-    }
-}
-
 // Up to 16 rows of x, quantised as they are read.  A lane of the 16x16x128 instruction
 // holds row lane % 16, columns 32 (lane / 16) on: exactly one block, so its scale
 // needs no other lane.  A workgroup takes 16 rows of the weight, its four waves a
@@ -301,8 +269,9 @@ __global__ void __launch_bounds__(kBlock) mx_tokens_kernel(MatrixView x, Mx4 w, 
 // Zeros where there is nothing to add up.
 template <bool BF16>
 __global__ void __launch_bounds__(kBlock) zero_matrix_kernel(MatrixOut out) {
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i < out.rows * out.cols) store_one<BF16>(out.data, i / out.cols * out.stride + i % out.cols, 0.f);
+    const int64_t n = out.rows * out.cols;
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlock)
+        store_one<BF16>(out.data, i / out.cols * out.stride + i % out.cols, 0.f);
 }
 
 hipError_t launch_mx_quantize(bool bf16, const MatrixView& x, const Mx4* q, const Mx4* qt, hipStream_t s);

@@ -171,6 +171,28 @@ def test_matmul(ctx, m, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(2000, 1500, 300), (1999, 1501, 129), (2049, 1409, 640), (1700, 1931, 20), (3300, 3800, 1200),
+                                   (3301, 3799, 1281), (3299, 3841, 2100)])
+def test_matmul_large_tiles(ctx, m, n, k, dtype):
+    """Sizes that take 128 x 128 and 256 x 256 tiles, ragged in every direction; the float64 product on the GPU."""
+    rng = np.random.default_rng(m + n + k)
+    x = (rng.normal(0, 1, (m, k)) * np.exp2(rng.integers(-6, 6, (m, 1)))).astype(np.float32)
+    w = rng.normal(0, 0.02, (n, k)).astype(np.float32)
+    xq, wq = al.Mxfp4.empty(m, k), al.Mxfp4.empty(n, k)
+    al.autoloco_mxfp4_quantize(ctx, torch.from_numpy(x).cuda(), xq)
+    al.autoloco_mxfp4_quantize(ctx, torch.from_numpy(w).cuda(), wq)
+    guard = torch.full((m + 2, n + 5), -77.0, dtype=DT[dtype], device="cuda")
+    out = guard[1:m + 1, 3:n + 3]
+    al.autoloco_mxfp4_matmul(ctx, xq, wq, out)
+    a, b = (torch.from_numpy(omx.rounded(v)).cuda() for v in (x, w))
+    ref, bound = a @ b.t().contiguous(), (k / 16 + 8) * 2.0 ** -23 * (a.abs() @ b.abs().t().contiguous())
+    assert torch.all((ref - bound).to(DT[dtype]) <= out) and torch.all(out <= (ref + bound).to(DT[dtype]))
+    inside = torch.zeros_like(guard, dtype=torch.bool)
+    inside[1:m + 1, 3:n + 3] = True
+    assert torch.all(guard[~inside] == -77.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 16, 128), (1, 1000, 2048), (2, 33, 31), (3, 100, 4100), (8, 257, 515), (13, 4099, 640),
                                    (15, 48, 127), (16, 64, 1024), (16, 5000, 260), (17, 300, 515), (33, 70, 1000)])
 def test_linear(ctx, m, n, k, dtype):
