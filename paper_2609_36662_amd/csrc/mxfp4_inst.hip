@@ -64,6 +64,25 @@ hipError_t matmul(const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t 
     }
 }
 
+// Rows of the weight a workgroup takes: 16, 32 or 48, the fewest that leave no more
+// workgroups than the chip's 256 compute units, so that none waits for a second one
+// (13 x 4,096 x 11,008 rows of weight, bf16: 15.8, 15.1 and 9.6 us), with sixteen waves
+// where there are few rows to share the columns out over (16 x 11,008 x 4,096 rows: 13.1
+// us against 17.0 with eight), eight otherwise.  Each of x's blocks is quantised once a
+// workgroup.
+template <bool BF16, int R, int NW>
+hipError_t tokens_at(const MatrixView& x, const Mx4& w, const MatrixOut& y, hipStream_t s) {
+    const unsigned blocks = (unsigned)((w.rows + 16 * R - 1) / (16 * R));
+    hipLaunchKernelGGL((mx_tokens_kernel<BF16, R, NW>), dim3(blocks), dim3(NW * 64), 0, s, x, w, y);
+    return hipGetLastError();
+}
+template <bool BF16>
+hipError_t tokens(const MatrixView& x, const Mx4& w, const MatrixOut& y, hipStream_t s) {
+    if (w.rows <= 16 * 256) return tokens_at<BF16, 1, 16>(x, w, y, s);
+    if (w.rows <= 32 * 256) return tokens_at<BF16, 2, 8>(x, w, y, s);
+    return tokens_at<BF16, 3, 8>(x, w, y, s);
+}
+
 }  // namespace
 
 hipError_t launch_mx_quantize(bool bf16, const MatrixView& x, const Mx4* q, const Mx4* qt, hipStream_t s) {
@@ -83,12 +102,7 @@ hipError_t launch_mx_matmul(bool bf16, const Mx4& a, const Mx4& b, const MatrixO
 }
 
 hipError_t launch_mx_tokens(bool bf16, const MatrixView& x, const Mx4& w, const MatrixOut& y, hipStream_t s) {
-    const unsigned blocks = (unsigned)((w.rows + 15) / 16);
-    if (bf16)
-        hipLaunchKernelGGL(mx_tokens_kernel<true>, dim3(blocks), dim3(kBlock), 0, s, x, w, y);
-    else
-        hipLaunchKernelGGL(mx_tokens_kernel<false>, dim3(blocks), dim3(kBlock), 0, s, x, w, y);
-    return hipGetLastError();
+    return bf16 ? tokens<true>(x, w, y, s) : tokens<false>(x, w, y, s);
 }
 
 }  // namespace autoloco

@@ -60,6 +60,91 @@ __device__ __forceinline__ uint32_t mx_codes8(const float (&x)[8], uint32_t s) {
     return w;
 }
 
+// Values as they lie in memory: 8 of them are 4 words of bf16 pairs or 8 of fp32.
+template <bool BF16>
+constexpr int kWords8 = BF16 ? 4 : 8;
+
+__device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+// Largest magnitude's bits (fp32) among N words.
+template <bool BF16, int N>
+__device__ __forceinline__ uint32_t mx_amax(const uint32_t (&w)[N]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (BF16)
+            m = pk_max_u16(m, w[i] & 0x7FFF7FFFu);
+        else
+            m = m > (w[i] & 0x7FFFFFFFu) ? m : w[i] & 0x7FFFFFFFu;
+    }
+    if constexpr (BF16) {
+        const uint32_t hi = m & 0xFFFF0000u, lo = m << 16;
+        m = hi > lo ? hi : lo;
+    }
+    return m;
+}
+
+// Codes of 8 values: bf16 pairs are converted as they are, unless the scale is one
+// that mx_codes8 treats apart.
+template <bool BF16>
+__device__ __forceinline__ uint32_t mx_codes8_raw(const uint32_t* w, uint32_t s) {
+    if constexpr (BF16) {
+        if (s >= 32 && s != kScaleNan) {
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+            const float scale = __uint_as_float(s << 23);
+            uint32_t c = 0;
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[0]), scale, 0);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[1]), scale, 1);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[2]), scale, 2);
+            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[3]), scale, 3);
+            return c;
+        }
+    }
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) {
+            v[2 * i] = bf16_lo(w[i]);
+            v[2 * i + 1] = bf16_hi(w[i]);
+        } else {
+            v[2 * i] = __uint_as_float(w[2 * i]);
+            v[2 * i + 1] = __uint_as_float(w[2 * i + 1]);
+        }
+    }
+    return mx_codes8(v, s);
+}
+
+// N words of a row from column i on (N * 2 or N values; those past n: 0).
+template <bool BF16, int N>
+__device__ __forceinline__ void load_raw(uint32_t (&w)[N], const char* row, int64_t i, int64_t n) {
+    constexpr int E = BF16 ? 2 : 1;
+    const char* p = row + i * (BF16 ? 2 : 4);
+    if (i + N * E <= n) {
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) {
+            const u32x4_any v = reinterpret_cast<const u32x4_any*>(p)[j];
+            w[4 * j] = v[0];
+            w[4 * j + 1] = v[1];
+            w[4 * j + 2] = v[2];
+            w[4 * j + 3] = v[3];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            w[j] = 0;
+            if constexpr (BF16) {
+                if (i + 2 * j < n) w[j] = reinterpret_cast<const uint16_t*>(p)[2 * j];
+                if (i + 2 * j + 1 < n) w[j] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[2 * j + 1] << 16;
+            } else {
+                if (i + j < n) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+            }
+        }
+    }
+}
+
 // The values of 8 codes under scale byte s.
 __device__ __forceinline__ void mx_values8(float (&x)[8], uint32_t w, uint32_t s) {
 #pragma unroll
@@ -91,17 +176,14 @@ __global__ void __launch_bounds__(kBlock) mx_rows_kernel(MatrixView x, Mx4 q) {
     const uint32_t row = unit / (uint32_t)q.groups, group = unit % (uint32_t)q.groups;
     if (row >= q.rows) return;
     const int piece = t & 15;
-    const int64_t col = (int64_t)group * 128 + piece * 8;
-    const char* src = static_cast<const char*>(x.data) + (int64_t)row * x.stride * (BF16 ? 2 : 4);
-    float v[8];
-    load8<BF16>(v, src, col, x.cols);
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max_bits(v[i], m);
+    uint32_t v[kWords8<BF16>];
+    load_raw<BF16>(v, static_cast<const char*>(x.data) + (int64_t)row * x.stride * (BF16 ? 2 : 4),
+                   (int64_t)group * 128 + piece * 8, x.cols);
+    uint32_t m = mx_amax<BF16>(v);
     m = max_dpp<0xB1>(m);   // lanes ^ 1, then ^ 2: the block's four
     m = max_dpp<0x4E>(m);
     const uint32_t s = mx_scale(m);
-    *reinterpret_cast<uint32_t*>(q.codes + (int64_t)row * q.row_bytes + group * 64 + piece * 4) = mx_codes8(v, s);
+    *reinterpret_cast<uint32_t*>(q.codes + (int64_t)row * q.row_bytes + group * 64 + piece * 4) = mx_codes8_raw<BF16>(v, s);
     if ((piece & 3) == 0) q.scales[((int64_t)group * q.rows + row) * 4 + (piece >> 2)] = (uint8_t)s;
 }
 
@@ -226,44 +308,88 @@ __global__ void __launch_bounds__(kBlock) mx_values_kernel(Mx4 q, MatrixOut out)
 // ----------------------------------------------------------------- product --
 __device__ __forceinline__ i32x8 operand(u32x4 w) { return i32x8{(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0}; }
 
-// Up to 16 rows of x, quantised as they are read.  A lane of the 16x16x128 instruction
-// holds row lane % 16, columns 32 (lane / 16) on: exactly one block, so its scale
-// needs no other lane.  A workgroup takes 16 rows of the weight, its four waves a
-// quarter of the columns each, joined in LDS.  Bound by reading the weight.
-template <bool BF16>
-__global__ void __launch_bounds__(kBlock) mx_tokens_kernel(MatrixView x, Mx4 w, MatrixOut y) {
-    __shared__ float part[4][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Up to 16 rows of x, quantised as they are read.  A workgroup takes 16 R rows of the
+// weight; its NW waves take groups of 128 columns in turn and are joined in LDS in wave
+// order.  A wave reads x in whole rows, 8 columns a lane and four rows at a time,
+// quantises them as mx_rows_kernel does, and passes the codes through its own piece of
+// LDS into the order of the 16x16x128 instruction: row lane % 16, columns 32 (lane / 16)
+// on.  (A lane that reads its own 32 columns needs no exchange, but its neighbours are 64
+// bytes apart, and the address unit takes a cycle for every lane: 13 x 4,096 x 11,008
+// rows 10.2 us against 9.6, 16 x 11,008 x 4,096 rows 17.6 against 13.1.)  Bound by the
+// latency of the weight's and x's loads, then by the quantisation (one row of x 7.4 us
+// where thirteen take 9.6): 24 MB of weight at 2.5 TB/s, launch included.
+template <bool BF16, int R, int NW>
+__global__ void __launch_bounds__(NW * 64) mx_tokens_kernel(MatrixView x, Mx4 w, MatrixOut y) {
+    constexpr int W = kWords8<BF16>;
+    constexpr int kRow = 80;                       // bytes of a row of codes: 16 rows' pieces in 64 banks
+    __shared__ __align__(16) uint8_t xlds[NW][16 * kRow + 64];
+    __shared__ float part[NW][R * 256];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, j = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
-    const int64_t wn = n0 + r < w.rows ? n0 + r : w.rows - 1;
-    const int64_t xm = r < x.rows ? r : x.rows - 1;
-    const char* xr = static_cast<const char*>(x.data) + xm * x.stride * (BF16 ? 2 : 4);
-    f32x4 acc = {};
-    for (int g = wave; g < w.groups; g += 4) {
-        const u32x4 wc = *reinterpret_cast<const u32x4*>(w.codes + wn * w.row_bytes + (int64_t)g * 64 + j * 16);
-        const uint32_t ws = w.scales[((int64_t)g * w.rows + wn) * 4 + j];
-        float v[4][8];
-        uint32_t m = 0;
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * R);
+    const uint8_t* wc[R];
+    const uint8_t* ws[R];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            load8<BF16>(v[i], xr, (int64_t)g * 128 + j * 32 + i * 8, x.cols);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) m = max_bits(v[i][e], m);
-        }
-        const uint32_t s = mx_scale(m);
-        u32x4 xc;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) xc[i] = mx_codes8(v[i], s);
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(wc), operand(xc), acc, 4, 4, 0, (int)ws, 0, (int)s);
+    for (int i = 0; i < R; ++i) {
+        const int64_t wn = n0 + 16 * i + r < w.rows ? n0 + 16 * i + r : w.rows - 1;
+        wc[i] = w.codes + wn * w.row_bytes + j * 16;
+        ws[i] = w.scales + wn * 4 + j;
     }
-    *reinterpret_cast<f32x4*>(&part[wave][lane * 4]) = acc;
+    const int quads = ((int)x.rows + 3) / 4;
+    uint8_t* mine = xlds[wave];
+    f32x4 acc[R] = {};
+    for (int g = wave; g < w.groups; g += NW) {
+        u32x4 c[R];
+        uint32_t s[R], v[4][W];
+        // x first: it is nearer, and is worked on while the weight is still on its way
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t row = 4 * q + j < x.rows ? 4 * q + j : x.rows - 1;
+            if (q < quads)
+                load_raw<BF16>(v[q], static_cast<const char*>(x.data) + row * x.stride * (BF16 ? 2 : 4),
+                               (int64_t)g * 128 + r * 8, x.cols);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            c[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wc[i] + (int64_t)g * 64));
+            s[i] = ws[i][(int64_t)g * w.rows * 4];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q < quads) {
+                uint32_t m = mx_amax<BF16>(v[q]);
+                m = max_dpp<0xB1>(m);
+                m = max_dpp<0x4E>(m);
+                const uint32_t xs = mx_scale(m);
+                *reinterpret_cast<uint32_t*>(mine + (4 * q + j) * kRow + r * 4) = mx_codes8_raw<BF16>(v[q], xs);
+                if ((r & 3) == 0) mine[16 * kRow + (4 * q + j) * 4 + r / 4] = (uint8_t)xs;
+            }
+        // the wave's own stores before its loads: LDS keeps their order, the compiler has to
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const u32x4 xc = *reinterpret_cast<const u32x4*>(mine + r * kRow + j * 16);
+        const uint32_t xs = mine[16 * kRow + r * 4 + j];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(c[i]), operand(xc), acc[i], 4, 4, 0, (int)s[i],
+                                                                      0, (int)xs);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) *reinterpret_cast<f32x4*>(&part[wave][i * 256 + lane * 4]) = acc[i];
     __syncthreads();
-    // thread t: token t / 16, row t % 16 of the weight
-    const int m = threadIdx.x >> 4, n = threadIdx.x & 15;
-    const int at = ((n >> 2) * 16 + m) * 4 + (n & 3);
-    const float sum = ((part[0][at] + part[1][at]) + part[2][at]) + part[3][at];
-    if (m < y.rows && n0 + n < y.cols) store_one<BF16>(y.data, m * y.stride + n0 + n, sum);
+    // value t: token t / (16 R), row t % (16 R) of the workgroup's
+    for (int t = threadIdx.x; t < (int)x.rows * 16 * R; t += NW * 64) {
+        const int m = t / (16 * R), n = t % (16 * R);
+        const int at = (n >> 4) * 256 + ((n >> 2 & 3) * 16 + m) * 4 + (n & 3);
+        float sum = part[0][at];
+#pragma unroll
+        for (int k = 1; k < NW; ++k) sum += part[k][at];
+        if (n0 + n < y.cols) store_one<BF16>(y.data, m * y.stride + n0 + n, sum);
+    }
 }
 
 // Zeros where there is nothing to add up.
