@@ -224,6 +224,37 @@ def test_large_logits(ctx):
     _check(x, labels, off, ref, got, 1e-4, 0.0, 1.0, "f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [7, 50, 3001])
+def test_logits_at_the_ends_of_the_type(ctx, vocab, dtype):
+    """Rows of the type's lowest value are uniform; its highest value has all the probability; one finite logit among
+    -inf has probability 1; the lowest value beside ordinary ones has none, wherever it stands."""
+    lo, hi, inf = torch.finfo(DT[dtype]).min, torch.finfo(DT[dtype]).max, float("inf")
+    x, labels, off, ref = _inputs([3, 3], vocab, dtype, 11, mask=0.0)
+    x[0] = lo
+    x[1] = 0.0
+    x[1, 3] = hi
+    x[2] = -inf
+    x[2, 4] = 1.5
+    labels[1], labels[2] = 3, 4
+    x[4] = lo
+    x[4, 5] = 2.0
+    labels[4] = 5
+    x[5, ::2] = lo
+    labels[5] = 1
+    losses, logps, work, g = _run(ctx, x, labels, off, torch.zeros(2))
+    assert work[6].item() == pytest.approx(-np.log(vocab), rel=1e-6)
+    assert work[[7, 8, 10]].tolist() == [0.0, 0.0, 0.0]
+    w = work[-2:].tolist()
+    assert torch.isfinite(losses).all() and torch.isfinite(g).all()
+    flat = torch.full((vocab,), -w[0] / vocab)
+    flat[int(labels[0])] += w[0]
+    assert torch.allclose(g[0].float().cpu(), flat, rtol=2.0 ** -7, atol=1e-9)
+    assert not g[[1, 2, 4]].any() and not g[5, ::2].any()
+    want = opref.row_logps(x[5:6].double().numpy(), labels[5:6].numpy())[0]
+    assert work[11].item() == pytest.approx(float(want[0]), rel=1e-5)
+
+
 def test_offsets_past_32_bits(ctx):
     """Rows that begin beyond 2^32 elements of the matrix."""
     vocab, stride, rows = 40, (1 << 32) // 5 + 1, 8
