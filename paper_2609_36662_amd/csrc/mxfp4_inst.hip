@@ -25,28 +25,31 @@ hipError_t quantize(const MatrixView& x, const Mx4* q, const Mx4* qt, hipStream_
 }
 
 // Which tile a product takes: 256 x 256 (one workgroup a compute unit, the most products
-// for every byte read from LDS), 128 x 128 (two) or 64 x 64.  From the times of full and
-// begun rounds of the chip's 256 compute units, in microseconds for g groups of 128
-// columns.  Measured (256, 128 and 64): 4,096 x 4,096 x 4,096 40, 45 and 66 us; 4,096 x
-// 11,008 x 4,096 106, 120 and 179; 4,608 x 4,096 x 4,096 (a second round barely begun) 62,
-// 56 and 74; 2,304 x 4,096 x 4,096 32, 35 and 40; 1,003 x 50,257 x 768 61, 43 and 55;
-// 1,024 x 4,096 x 2,048 18.1, 8.8 and 10.9; 512 x 4,096 x 2,048 17.7, 8.0 and 7.2.
-enum Tile { TILE_256, TILE_128, TILE_64 };
+// for every byte read from LDS), 128 x 128 (two, or one with four stages on the way where
+// there are no more tiles than units and many columns) or 64 x 64.  From the times of full
+// and begun rounds of the chip's 256 compute units, in microseconds for g groups of 128
+// columns.  Measured (256, 128 and 64): 4,096 x 4,096 x 4,096 39, 40 and 59 us; 4,096 x
+// 11,008 x 4,096 110, 115 and 152; 4,608 x 4,096 x 4,096 (a second round barely begun) 61,
+// 49 and 65; 2,304 x 4,096 x 4,096 31, 31 and 35; 1,003 x 50,257 x 768 51, 40 and 48; 1,024 x
+// 4,096 x 2,048 18.5, 8.7 and 9.7; 512 x 4,096 x 2,048 17.7, 7.8 and 6.4; 2,048 x 2,048 x
+// 5,632 37, 19.6 (17.3 with four stages) and 21.5; 768 x 4,096 x 2,048 18.1, 8.3 (8.5) and 8.0.
+enum Tile { TILE_256, TILE_128, TILE_128_DEEP, TILE_64 };
 Tile tile_for(int64_t m, int64_t n, int32_t groups) {
     auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
     const double g = groups;
     const int64_t t256 = tiles(256), t128 = tiles(128);
-    if (t128 < 176) return TILE_64;
+    if (t128 < 224) return TILE_64;
     const int64_t full256 = t256 / 256, rest256 = t256 % 256, full128 = t128 / 512, rest128 = t128 % 512;
-    const double us256 = full256 * (0.94 * g + 9.0) + (rest256 > 0 ? 0.75 * g + 8.0 : 0.0);
-    const double us128 = full128 * (0.62 * g + 2.5) + (rest128 > 256 ? 0.5 * g + 2.5 : rest128 > 0 ? 0.3 * g + 2.0 : 0.0);
-    return us256 < us128 ? TILE_256 : TILE_128;
+    const double us256 = full256 * (0.85 * g + 9.0) + (rest256 > 0 ? 0.75 * g + 8.0 : 0.0);
+    const double us128 = full128 * (0.52 * g + 3.2) + (rest128 > 256 ? 0.45 * g + 3.0 : rest128 > 0 ? 0.3 * g + 2.0 : 0.0);
+    if (us256 < us128) return TILE_256;
+    return t128 <= 256 && groups >= 24 ? TILE_128_DEEP : TILE_128;
 }
 
-template <int T, bool BF16>
+template <int T, int ST, bool BF16>
 hipError_t tiles(const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t s) {
     const TileGrid g{(uint32_t)((out.rows + 64 * T - 1) / (64 * T)), (uint32_t)((out.cols + 64 * T - 1) / (64 * T))};
-    hipLaunchKernelGGL((mx_tile_kernel<T, BF16>), dim3(g.mt * g.nt), dim3(256), 0, s, a, b, out, g);
+    hipLaunchKernelGGL((mx_tile_kernel<T, ST, BF16>), dim3(g.mt * g.nt), dim3(256), 0, s, a, b, out, g);
     return hipGetLastError();
 }
 
@@ -58,9 +61,10 @@ hipError_t matmul(const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t 
         return hipGetLastError();
     }
     switch (tile_for(out.rows, out.cols, a.groups)) {
-        case TILE_256: return tiles<4, BF16>(a, b, out, s);
-        case TILE_128: return tiles<2, BF16>(a, b, out, s);
-        default: return tiles<1, BF16>(a, b, out, s);
+        case TILE_256: return tiles<4, 2, BF16>(a, b, out, s);
+        case TILE_128: return tiles<2, 2, BF16>(a, b, out, s);
+        case TILE_128_DEEP: return tiles<2, 4, BF16>(a, b, out, s);
+        default: return tiles<1, 2, BF16>(a, b, out, s);
     }
 }
 

@@ -171,7 +171,7 @@ def test_matmul(ctx, m, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("m,n,k", [(2000, 1500, 300), (1999, 1501, 129), (2049, 1409, 640), (1700, 1931, 20), (3300, 3800, 1200),
+@pytest.mark.parametrize("m,n,k", [(2000, 2040, 3100), (1999, 1921, 4000), (2000, 1500, 300), (1999, 1501, 129), (2049, 1409, 640), (1700, 1931, 20), (3300, 3800, 1200),
                                    (3301, 3799, 1281), (3299, 3841, 2100)])
 def test_matmul_large_tiles(ctx, m, n, k, dtype):
     """Sizes that take 128 x 128 and 256 x 256 tiles, ragged in every direction; the float64 product on the GPU."""
