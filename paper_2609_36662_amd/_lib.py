@@ -718,12 +718,13 @@ class Mxfp4:
 
     def __init__(self, rows: int, cols: int, codes, scales):
         import torch
-        groups = (cols + 127) // 128
-        for t, n, what in ((codes, rows * groups * 64, "codes"), (scales, rows * groups * 4, "scales")):
-            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.uint8 or not t.is_contiguous():
-                raise TypeError(f"{what} must be a contiguous CUDA (HIP) uint8 tensor")
-            if t.numel() != n:
-                raise ValueError(f"{what} of {rows} x {cols} takes {n} bytes, got {t.numel()}")
+        u8, units = torch.uint8, rows * ((cols + 127) // 128)
+        if codes.dtype is not u8 or scales.dtype is not u8 or not codes.is_cuda or not scales.is_cuda \
+                or not codes.is_contiguous() or not scales.is_contiguous():
+            raise TypeError("codes and scales must be contiguous CUDA (HIP) uint8 tensors")
+        if codes.numel() != 64 * units or scales.numel() != 4 * units:
+            raise ValueError(f"{rows} x {cols} takes {64 * units} bytes of codes and {4 * units} of scales, got "
+                             f"{codes.numel()} and {scales.numel()}")
         self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
         self.buffers = Mxfp4Buffers(rows, cols, codes.data_ptr(), scales.data_ptr())
 

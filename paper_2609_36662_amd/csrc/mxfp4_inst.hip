@@ -6,22 +6,34 @@ namespace autoloco {
 namespace {
 
 // Workgroups of kBlock threads, 16 of them a row's 128 columns.
-unsigned group_blocks(const Mx4& q) { return (unsigned)((q.rows * q.groups * 16 + kBlock - 1) / kBlock); }
+int64_t group_blocks(const Mx4& q) { return (q.rows * q.groups * 16 + kBlock - 1) / kBlock; }
+
+// launch(first, count) over all workgroups, at most 2^20 at a time.
+template <typename Launch>
+hipError_t in_slices(int64_t blocks, Launch launch) {
+    constexpr int64_t kSlice = int64_t(1) << 20;
+    for (int64_t first = 0; first < blocks; first += kSlice) {
+        launch((uint32_t)first, dim3((unsigned)(blocks - first < kSlice ? blocks - first : kSlice)));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 template <bool BF16>
 hipError_t quantize(const MatrixView& x, const Mx4* q, const Mx4* qt, hipStream_t s) {
-    if (qt == nullptr) {
-        hipLaunchKernelGGL(mx_rows_kernel<BF16>, dim3(group_blocks(*q)), dim3(kBlock), 0, s, x, *q);
-        return hipGetLastError();
-    }
+    if (qt == nullptr)
+        return in_slices(group_blocks(*q), [&](uint32_t first, dim3 grid) {
+            hipLaunchKernelGGL(mx_rows_kernel<BF16>, grid, dim3(kBlock), 0, s, x, *q, first);
+        });
     // whole groups of 128 columns, so that the padding is written too
     const uint32_t tiles = (uint32_t)((x.cols + 127) / 128) * (BF16 ? 1 : 2);
-    const uint32_t blocks = tiles * (uint32_t)((x.rows + 127) / 128);
-    if (q != nullptr)
-        hipLaunchKernelGGL((mx_cols_kernel<BF16, true>), dim3(blocks), dim3(kBlock), 0, s, x, *q, *qt, tiles);
-    else
-        hipLaunchKernelGGL((mx_cols_kernel<BF16, false>), dim3(blocks), dim3(kBlock), 0, s, x, *qt, *qt, tiles);
-    return hipGetLastError();
+    return in_slices(tiles * ((x.rows + 127) / 128), [&](uint32_t first, dim3 grid) {
+        if (q != nullptr)
+            hipLaunchKernelGGL((mx_cols_kernel<BF16, true>), grid, dim3(kBlock), 0, s, x, *q, *qt, tiles, first);
+        else
+            hipLaunchKernelGGL((mx_cols_kernel<BF16, false>), grid, dim3(kBlock), 0, s, x, *qt, *qt, tiles, first);
+    });
 }
 
 // Which tile a product takes: 256 x 256 (one workgroup a compute unit, the most products
@@ -94,11 +106,12 @@ hipError_t launch_mx_quantize(bool bf16, const MatrixView& x, const Mx4* q, cons
 }
 
 hipError_t launch_mx_values(bool bf16, const Mx4& q, const MatrixOut& out, hipStream_t s) {
-    if (bf16)
-        hipLaunchKernelGGL(mx_values_kernel<true>, dim3(group_blocks(q)), dim3(kBlock), 0, s, q, out);
-    else
-        hipLaunchKernelGGL(mx_values_kernel<false>, dim3(group_blocks(q)), dim3(kBlock), 0, s, q, out);
-    return hipGetLastError();
+    return in_slices(group_blocks(q), [&](uint32_t first, dim3 grid) {
+        if (bf16)
+            hipLaunchKernelGGL(mx_values_kernel<true>, grid, dim3(kBlock), 0, s, q, out, first);
+        else
+            hipLaunchKernelGGL(mx_values_kernel<false>, grid, dim3(kBlock), 0, s, q, out, first);
+    });
 }
 
 hipError_t launch_mx_matmul(bool bf16, const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t s) {

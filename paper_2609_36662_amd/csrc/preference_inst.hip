@@ -12,29 +12,41 @@ namespace {
 // with 256 in both, 502 so).
 constexpr int64_t kFewRows = 512;
 
+// launch(first, count) over all rows (and pairs), at most 2^20 at a time.
+template <typename Launch>
+hipError_t in_slices(int64_t rows, Launch launch) {
+    constexpr int64_t kSlice = int64_t(1) << 20;
+    for (int64_t first = 0; first < rows; first += kSlice) {
+        launch(first, dim3((unsigned)(rows - first < kSlice ? rows - first : kSlice)));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <bool BF16>
 hipError_t row_logp(const SequenceArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)a.logits.rows);
-    if (a.logits.rows <= kFewRows)
-        hipLaunchKernelGGL((row_logp_kernel<BF16, 1024>), grid, dim3(1024), 0, s, a);
-    else
-        hipLaunchKernelGGL((row_logp_kernel<BF16, 256>), grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+    return in_slices(a.logits.rows, [&](int64_t first, dim3 grid) {
+        if (a.logits.rows <= kFewRows)
+            hipLaunchKernelGGL((row_logp_kernel<BF16, 1024>), grid, dim3(1024), 0, s, a, first);
+        else
+            hipLaunchKernelGGL((row_logp_kernel<BF16, 256>), grid, dim3(256), 0, s, a, first);
+    });
 }
 
 template <bool BF16>
 hipError_t logit_grad(bool pairs, const SequenceArgs& a, const PreferenceArgs& p, const MatrixOut& g, hipStream_t s) {
-    const dim3 grid((unsigned)(a.logits.rows + (pairs ? a.sequences / 2 : 0)));
     const bool few = a.logits.rows <= kFewRows;
-    if (few && pairs)
-        hipLaunchKernelGGL((logit_grad_kernel<BF16, 1024, true>), grid, dim3(1024), 0, s, a, p, g);
-    else if (few)
-        hipLaunchKernelGGL((logit_grad_kernel<BF16, 1024, false>), grid, dim3(1024), 0, s, a, p, g);
-    else if (pairs)
-        hipLaunchKernelGGL((logit_grad_kernel<BF16, 512, true>), grid, dim3(512), 0, s, a, p, g);
-    else
-        hipLaunchKernelGGL((logit_grad_kernel<BF16, 512, false>), grid, dim3(512), 0, s, a, p, g);
-    return hipGetLastError();
+    return in_slices(a.logits.rows + (pairs ? a.sequences / 2 : 0), [&](int64_t first, dim3 grid) {
+        if (few && pairs)
+            hipLaunchKernelGGL((logit_grad_kernel<BF16, 1024, true>), grid, dim3(1024), 0, s, a, p, g, first);
+        else if (few)
+            hipLaunchKernelGGL((logit_grad_kernel<BF16, 1024, false>), grid, dim3(1024), 0, s, a, p, g, first);
+        else if (pairs)
+            hipLaunchKernelGGL((logit_grad_kernel<BF16, 512, true>), grid, dim3(512), 0, s, a, p, g, first);
+        else
+            hipLaunchKernelGGL((logit_grad_kernel<BF16, 512, false>), grid, dim3(512), 0, s, a, p, g, first);
+    });
 }
 
 }  // namespace

@@ -180,13 +180,14 @@ __device__ __forceinline__ RunningSum<PLAIN> row_sum(const char* x, int64_t voca
     return r;
 }
 
-// Each row's log sum exp and its label's log-probability; a workgroup a row.  Bound by
+// Each row's log sum exp and its label's log-probability; a workgroup a row (first: the
+// launch's first row, since a grid has fewer than 2^32 threads).  Bound by
 // HBM with fp32 logits; with bf16 ones the exponentials (a quarter of the rate of other
 // instructions) take as long as the reading.
 template <bool BF16, int NT>
-__global__ void __launch_bounds__(NT) row_logp_kernel(SequenceArgs a) {
+__global__ void __launch_bounds__(NT) row_logp_kernel(SequenceArgs a, int64_t first) {
     __shared__ float lds[2 * (NT / 64)];
-    const int64_t row = blockIdx.x;
+    const int64_t row = first + blockIdx.x;
     const int64_t label = live_label(a, row);
     if (label < 0) {
         if (threadIdx.x == 0) {
@@ -344,9 +345,9 @@ __device__ __forceinline__ void row_gradient(const char* x, char* out, int64_t v
 // logits.  PAIRS: there was no pair kernel; each workgroup finds its pair's weight
 // itself, and one more workgroup a pair, at the end, writes its outputs.
 template <bool BF16, int NT, bool PAIRS>
-__global__ void __launch_bounds__(NT) logit_grad_kernel(SequenceArgs a, PreferenceArgs p, MatrixOut g) {
+__global__ void __launch_bounds__(NT) logit_grad_kernel(SequenceArgs a, PreferenceArgs p, MatrixOut g, int64_t first) {
     __shared__ double lds[NT / 64];
-    const int64_t row = blockIdx.x;
+    const int64_t row = first + blockIdx.x;
     if constexpr (PAIRS) {
         if (row >= a.logits.rows) {
             pair_outputs<NT>(a, p, row - a.logits.rows, lds);
