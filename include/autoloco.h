@@ -532,7 +532,7 @@ int autoloco_mxfp4_dequantize(autoloco_ctx* ctx, const autoloco_mxfp4* q, const 
 int autoloco_mxfp4_matmul(autoloco_ctx* ctx, const autoloco_mxfp4* a, const autoloco_mxfp4* b,
                           const autoloco_matrix* out);
 /* y = x W^T with x quantised on the way (the values are those of quantize and
- * matmul).  Up to AUTOLOCO_MXFP4_TOKENS rows (tokens being decoded) x is quantised
+ * matmul, which also give a y of another dtype than x's).  Up to AUTOLOCO_MXFP4_TOKENS rows (tokens being decoded) x is quantised
  * inside the product and xq is not used (may be NULL); beyond, xq (x's shape)
  * receives x's 4-bit form.  Asynchronous.  Errors: as above. */
 #define AUTOLOCO_MXFP4_TOKENS 16

@@ -23,7 +23,10 @@
 
 namespace autoloco {
 
-constexpr int kChunk = 16384;
+// Elements of a chunk; of a small list, whose chunks are no more than the chip's
+// workgroups, fewer.
+constexpr int kChunk = 16384, kSmallChunk = 4096;
+constexpr int64_t kSmallList = int64_t(16) << 20;
 
 // One chunk of a gradient tensor: n elements at grad, to packed (or grad itself).
 struct GradChunk {
@@ -161,6 +164,11 @@ __device__ __forceinline__ void chunk_scale(const GradChunk& c, float coef) {
 [[maybe_unused]] static __global__ void __launch_bounds__(kBlock) tensor_clip_kernel(ClipArgs a) {
     __shared__ double total;
     const int k = blockIdx.y;
+    // From the last chunk down: what the caches still hold of the first pass comes first.
+    const int64_t begin = a.first[k];
+    int64_t i = a.first[k + 1] - 1 - blockIdx.x;
+    GradChunk c{};
+    if (i >= begin) c = a.chunks[i];   // on its way while the sums are added up
     double t[1] = {0.0};
     for (int b = threadIdx.x; b < (int)gridDim.x; b += kBlock) t[0] += a.partials[(int64_t)k * gridDim.x + b];
     const double sum = block_reduce<1, kBlock>(t);
@@ -174,11 +182,7 @@ __device__ __forceinline__ void chunk_scale(const GradChunk& c, float coef) {
     }
     __syncthreads();
     const float coef = a.max_norm > 0.0 ? clip_coef(total, a.max_norm) : 1.0f;
-    // From the last chunk down: what the caches still hold of the first pass comes first.
-    const int64_t begin = a.first[k];
-    int64_t i = a.first[k + 1] - 1 - blockIdx.x;
     if (i < begin) return;
-    GradChunk c = a.chunks[i];
     if (c.packed == nullptr && coef == 1.0f) return;   // nothing to change in place
     for (;;) {
         i -= gridDim.x;

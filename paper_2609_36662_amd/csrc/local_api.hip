@@ -337,12 +337,14 @@ int autoloco_grads_create(autoloco_ctx* c, const autoloco_grad* t, int64_t count
         if (workers < 1 || workers > AUTOLOCO_MAX_K) return fail(c, AUTOLOCO_E_INVALID, "workers outside 1..16");
         std::vector<Range> ranges;
         bool packs = false;
+        int64_t total = 0;
         for (int64_t i = 0; i < count; ++i) {
             if (t[i].dtype != AUTOLOCO_F32 && t[i].dtype != AUTOLOCO_BF16)
                 return fail(c, AUTOLOCO_E_INVALID, "unknown dtype of a gradient");
             if (t[i].n < 0 || t[i].n > (int64_t(1) << 40)) return fail(c, AUTOLOCO_E_INVALID, "n of a gradient outside 0..2^40");
             if (t[i].worker < 0 || t[i].worker >= workers) return fail(c, AUTOLOCO_E_INVALID, "a gradient of no worker");
             if (t[i].n == 0) continue;
+            total += t[i].n;
             if (ranges.empty()) packs = t[i].packed != nullptr;
             if ((t[i].packed != nullptr) != packs) return fail(c, AUTOLOCO_E_INVALID, "packed set for some gradients only");
             const uintptr_t g = reinterpret_cast<uintptr_t>(t[i].grad), p = reinterpret_cast<uintptr_t>(t[i].packed);
@@ -365,16 +367,17 @@ int autoloco_grads_create(autoloco_ctx* c, const autoloco_grad* t, int64_t count
         autoloco_grads list;
         list.device = c->device;
         list.workers = workers;
+        const int64_t chunk = total <= kSmallList ? kSmallChunk : kChunk;
         std::vector<GradChunk> chunks;
         for (int32_t k = 0; k < workers; ++k) {
             list.first[k] = static_cast<int64_t>(chunks.size());
             for (int64_t i = 0; i < count; ++i) {
                 if (t[i].worker != k) continue;
-                for (int64_t at = 0; at < t[i].n; at += kChunk) {
+                for (int64_t at = 0; at < t[i].n; at += chunk) {
                     GradChunk ch{};
                     ch.grad = static_cast<char*>(t[i].grad) + at * element_size(t[i].dtype);
                     ch.packed = packs ? t[i].packed + at : nullptr;
-                    ch.n = static_cast<int32_t>(std::min<int64_t>(kChunk, t[i].n - at));
+                    ch.n = static_cast<int32_t>(std::min<int64_t>(chunk, t[i].n - at));
                     ch.bf16 = t[i].dtype == AUTOLOCO_BF16;
                     chunks.push_back(ch);
                 }

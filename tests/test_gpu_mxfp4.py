@@ -241,6 +241,58 @@ def test_gradients_of_a_layer(ctx, dtype):
         assert abs(diff - float(dw[i, j])) <= 1e-9 + (m / 16 + 8) * 2.0 ** -23 * np.sum(np.abs(dr[:, i] * xr[:, j])) * 2
 
 
+def test_codes_past_32_bits(ctx):
+    """More than 2^32 bytes of codes, from one row broadcast: every row of the form is the first one's, and a product
+    with it has equal columns."""
+    rows, cols = 70001, 131072
+    row = torch.randn(1, cols, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    q = al.Mxfp4.empty(rows, cols)
+    q.codes[-1].fill_(0xA5)
+    al.autoloco_mxfp4_quantize(ctx, row.expand(rows, cols), q)
+    codes, scales = omx.pack(*omx.quantize(row.double().cpu().numpy()))
+    want, wants = torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()
+    for a in range(0, rows, 10000):
+        assert torch.equal(q.codes[a:a + 10000], q.codes[:1].expand(min(10000, rows - a), -1))
+    _codes_equal(q.codes[-1:].cpu().numpy(), want.cpu().numpy())
+    assert torch.equal(q.scales, wants.expand(-1, rows, -1))
+    for m in (5, 40):
+        x = torch.randn(m, cols, device="cuda")
+        y, xq = torch.empty((m, rows), device="cuda"), al.Mxfp4.empty(m, cols)
+        al.autoloco_mxfp4_linear(ctx, x, q, y, xq)
+        assert torch.equal(y, y[:, :1].expand(m, rows))
+        _check_product(y[:, -1:], omx.rounded(x.double().cpu().numpy()), omx.rounded(row.double().cpu().numpy()), "f32", cols)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides_past_32_bits(ctx, dtype):
+    """Rows of x and of the results that begin beyond 2^32 bytes."""
+    rows, cols, stride = 21, 150, (1 << 28) + 3
+    store = torch.empty(stride * (rows - 1) + cols, dtype=DT[dtype], device="cuda")
+    x = torch.as_strided(store, (rows, cols), (stride, 1))
+    x.copy_(torch.randn(rows, cols))
+    q, qt = al.Mxfp4.empty(rows, cols), al.Mxfp4.empty(cols, rows)
+    al.autoloco_mxfp4_quantize(ctx, x, q, qt)
+    ref = x.double().cpu().numpy()
+    for m, r in ((q, ref), (qt, ref.T)):
+        codes, scales = omx.pack(*omx.quantize(r))
+        assert np.array_equal(m.scales.cpu().numpy(), scales)
+        _codes_equal(m.codes.cpu().numpy(), codes)
+    w = al.Mxfp4.empty(cols, cols)
+    wv = np.random.default_rng(2).normal(0, 1, (cols, cols)).astype(np.float32)
+    al.autoloco_mxfp4_quantize(ctx, torch.from_numpy(wv).cuda(), w)
+    for m in (rows, 9):
+        y = torch.empty((m, cols), dtype=DT[dtype], device="cuda")
+        al.autoloco_mxfp4_linear(ctx, x[:m], w, y, al.Mxfp4.empty(m, cols))
+        _check_product(y, omx.rounded(ref[:m]), omx.rounded(wv), dtype, cols)
+    y = x[:9].clone()
+    al.autoloco_mxfp4_linear(ctx, y, w, x[9:18])
+    _check_product(x[9:18], omx.rounded(ref[:9]), omx.rounded(wv), dtype, cols)
+    al.autoloco_mxfp4_matmul(ctx, q, w, x)
+    _check_product(x, omx.rounded(ref), omx.rounded(wv), dtype, cols)
+    al.autoloco_mxfp4_dequantize(ctx, q, x)
+    assert np.array_equal(x.double().cpu().numpy(), omx.rounded(ref))
+
+
 def test_empty_matrices(ctx):
     e = al.Mxfp4.empty
     for rows, cols in ((0, 5), (5, 0), (0, 0)):

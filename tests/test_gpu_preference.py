@@ -266,6 +266,26 @@ def test_offsets_past_32_bits(ctx):
     _check(x, labels, off, ref, got, 0.1, 0.0, 1.0, "bf16")
 
 
+def test_more_rows_than_one_launch(ctx):
+    """A million and a half rows, one row of logits broadcast."""
+    n, vocab = 1_500_000, 3
+    x = torch.tensor([[0.5, -1.0, 2.0]], device="cuda").expand(n, vocab)
+    labels = torch.zeros(n, dtype=torch.int64)
+    off, ref = torch.tensor([0, 700_000, n]), torch.tensor([0.0, 0.0])
+    g = torch.full((n, vocab), 9.0, device="cuda")
+    losses, logps, work, _ = _run(ctx, x, labels, off, ref, grads=g, beta=1e-7)
+    v = np.array([0.5, -1.0, 2.0])
+    lse = np.log(np.exp(v).sum())
+    z = 1e-7 * (0.5 - lse) * (700_000 - 800_000)
+    assert logps.tolist() == pytest.approx([(0.5 - lse) * 700_000, (0.5 - lse) * 800_000], rel=1e-6)
+    assert float(losses[0]) == pytest.approx(np.log1p(np.exp(-z)), rel=1e-6)
+    w = 1e-7 * (1 / (1 + np.exp(-z)) - 1)
+    want = w * ((np.arange(3) == 0) - np.exp(v - lse))
+    for a, b, s in ((0, 700_000, 1), (700_000, n, -1)):
+        assert torch.equal(g[a:b], g[a:a + 1].expand(b - a, vocab))
+        np.testing.assert_allclose(g[a].cpu().numpy(), s * want, rtol=1e-5)
+
+
 def test_no_rows_and_no_pairs(ctx):
     e = torch.empty
     got = _run(ctx, e(0, 10), e(0, dtype=torch.int64), torch.zeros(3, dtype=torch.int64), torch.tensor([1.0, 2.0]), beta=0.5)
