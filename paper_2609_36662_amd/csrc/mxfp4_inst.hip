@@ -45,15 +45,21 @@ hipError_t quantize(const MatrixView& x, const Mx4* q, const Mx4* qt, hipStream_
 // 49 and 65; 2,304 x 4,096 x 4,096 31, 31 and 35; 1,003 x 50,257 x 768 51, 40 and 48; 1,024 x
 // 4,096 x 2,048 18.5, 8.7 and 9.7; 512 x 4,096 x 2,048 17.7, 7.8 and 6.4; 2,048 x 2,048 x
 // 5,632 37, 19.6 (17.3 with four stages) and 21.5; 768 x 4,096 x 2,048 18.1, 8.3 (8.5) and 8.0.
+// Those times are of bf16 results on operands and results that the caches hold.  Where
+// they come from memory and large fp32 results go there, the wider tile's longer runs of a
+// row count for more (256 and 128): 1,003 x 50,257 x 768 77 and 86 us, 1,024 x 32,768 x
+// 768 47 and 55, 2,048 x 32,000 x 2,048 111 and 137 (bf16 results 54 and 61, 31 and 27,
+// 94 and 109): a tenth of a microsecond for every megabyte.
 enum Tile { TILE_256, TILE_128, TILE_128_DEEP, TILE_64 };
-Tile tile_for(int64_t m, int64_t n, int32_t groups) {
+Tile tile_for(int64_t m, int64_t n, int32_t groups, bool bf16) {
     auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
     const double g = groups;
     const int64_t t256 = tiles(256), t128 = tiles(128);
     if (t128 < 224) return TILE_64;
     const int64_t full256 = t256 / 256, rest256 = t256 % 256, full128 = t128 / 512, rest128 = t128 % 512;
     const double us256 = full256 * (0.85 * g + 9.0) + (rest256 > 0 ? 0.75 * g + 8.0 : 0.0);
-    const double us128 = full128 * (0.52 * g + 3.2) + (rest128 > 256 ? 0.45 * g + 3.0 : rest128 > 0 ? 0.3 * g + 2.0 : 0.0);
+    const double us128 = full128 * (0.52 * g + 3.2) + (rest128 > 256 ? 0.45 * g + 3.0 : rest128 > 0 ? 0.3 * g + 2.0 : 0.0) +
+                         (bf16 ? 0.0 : 4e-7 * static_cast<double>(m) * static_cast<double>(n));
     if (us256 < us128) return TILE_256;
     return t128 <= 256 && groups >= 24 ? TILE_128_DEEP : TILE_128;
 }
@@ -72,7 +78,7 @@ hipError_t matmul(const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t 
         hipLaunchKernelGGL(zero_matrix_kernel<BF16>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(kBlock), 0, s, out);
         return hipGetLastError();
     }
-    switch (tile_for(out.rows, out.cols, a.groups)) {
+    switch (tile_for(out.rows, out.cols, a.groups, BF16)) {
         case TILE_256: return tiles<4, 2, BF16>(a, b, out, s);
         case TILE_128: return tiles<2, 2, BF16>(a, b, out, s);
         case TILE_128_DEEP: return tiles<2, 4, BF16>(a, b, out, s);
