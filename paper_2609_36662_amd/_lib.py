@@ -771,13 +771,14 @@ def make_sequences(logits, labels, offsets, work) -> Sequences:
     offsets [sequences + 1] int64, work at least 2 rows + sequences float32."""
     import torch
     m = make_matrix(logits, "logits")
+    i64, f32 = torch.int64, torch.float32
+    if labels.dtype is not i64 or offsets.dtype is not i64 or work.dtype is not f32 or not labels.is_cuda \
+            or not offsets.is_cuda or not work.is_cuda or not labels.is_contiguous() or not offsets.is_contiguous() \
+            or not work.is_contiguous():
+        raise TypeError("labels and offsets must be contiguous CUDA (HIP) int64 tensors and work a float32 one")
     rows, count = m.rows, offsets.numel() - 1
-    for t, dtype, n, what in ((labels, torch.int64, rows, "labels"), (offsets, torch.int64, 1, "offsets"),
-                              (work, torch.float32, 2 * rows + count, "work")):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype or not t.is_contiguous():
-            raise TypeError(f"{what} must be a contiguous CUDA (HIP) {dtype} tensor")
-        if t.numel() < n:
-            raise ValueError(f"{what} is shorter than {n}")
+    if count < 0 or labels.numel() < rows or work.numel() < 2 * rows + count:
+        raise ValueError(f"{rows} rows and {count} sequences need {rows} labels, an offset and {2 * rows + count} values of work")
     return Sequences(m, labels.data_ptr(), offsets.data_ptr(), count, work.data_ptr())
 
 

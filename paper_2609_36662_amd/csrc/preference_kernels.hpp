@@ -52,9 +52,10 @@ __device__ __forceinline__ int64_t offset_at(const SequenceArgs& a, int64_t i) {
 
 // The label of a row, or -1 if the row is masked.
 __device__ __forceinline__ int64_t live_label(const SequenceArgs& a, int64_t row) {
-    const int64_t l = a.labels[row];
-    if (l < 0 || l >= a.logits.cols || a.sequences == 0) return -1;
-    return row >= offset_at(a, 0) && row < offset_at(a, a.sequences) ? l : -1;
+    if (a.sequences == 0) return -1;
+    // all three on their way together
+    const int64_t l = a.labels[row], lo = offset_at(a, 0), hi = offset_at(a, a.sequences);
+    return l >= 0 && l < a.logits.cols && row >= lo && row < hi ? l : -1;
 }
 
 // A row seen as a head of single elements up to a 16-byte boundary, vectors of 16 bytes
@@ -275,15 +276,16 @@ __global__ void __launch_bounds__(NT) pair_kernel(SequenceArgs a, PreferenceArgs
     pair_outputs<NT>(a, p, blockIdx.x, lds);
 }
 
-// The sequence that row belongs to: the last one that begins at or before it.
+// The sequence that row belongs to: the last one that begins at or before it.  A wave
+// looks at 64 of them at a time.
 __device__ __forceinline__ int64_t sequence_of(const SequenceArgs& a, int64_t row) {
-    int64_t lo = 0, hi = a.sequences - 1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) / 2;
-        if (offset_at(a, mid) <= row)
-            lo = mid;
-        else
-            hi = mid - 1;
+    int64_t lo = 0, n = a.sequences;
+    while (n > 1) {
+        const int64_t step = (n + 63) / 64, at = lo + (threadIdx.x & 63) * step;
+        const int begun = __popcll(__ballot(at < lo + n && offset_at(a, at < lo + n ? at : lo) <= row));
+        const int64_t end = lo + n;
+        if (begun > 1) lo += (begun - 1) * step;
+        n = end - lo < step ? end - lo : step;
     }
     return lo;
 }

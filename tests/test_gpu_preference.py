@@ -266,6 +266,14 @@ def test_offsets_past_32_bits(ctx):
     _check(x, labels, off, ref, got, 0.1, 0.0, 1.0, "bf16")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,vocab", [([400, 250], 8209), ([300, 0, 220, 170], 3001)])
+def test_many_long_rows(ctx, lens, vocab, dtype):
+    """More than 512 rows of more than 16 KB, and of 4 to 16 KB."""
+    t = _inputs(lens, vocab, dtype, 21)
+    _check(*t, _run(ctx, *t, smoothing=0.1), 0.1, 0.1, 1.0, dtype)
+
+
 def test_more_rows_than_one_launch(ctx):
     """A million and a half rows, one row of logits broadcast."""
     n, vocab = 1_500_000, 3
