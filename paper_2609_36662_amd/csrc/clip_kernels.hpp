@@ -48,17 +48,17 @@ struct ClipArgs {
 };
 
 // Chunks begin at any element: a head of single elements up to the boundary at which
-// vectors of V may begin, the vectors (four of a thread's in flight), and a tail.
-// whole(U, i): vectors i, i + kBlock, ... (U of them, an integral_constant);
-// single(j): element j.
-template <int V, typename Whole, typename Single>
-__device__ __forceinline__ void over_chunk(const void* boundary, int element, int n, Whole whole, Single single) {
+// vectors of V may begin, the vectors (four of a thread's in flight, the last ones too),
+// and a tail.  four(whole, head, i, n): vectors i, i + kBlock, i + 2 kBlock, i + 3 kBlock, all there if
+// whole (a constant), else those below n; single(j): element j.
+template <int V, typename Four, typename Single>
+__device__ __forceinline__ void over_chunk(const void* boundary, int element, int n, Four four, Single single) {
     const int off = (int)(reinterpret_cast<uintptr_t>(boundary) / element % V);
     const int head = off == 0 ? 0 : V - off < n ? V - off : n;
     const int vectors = (n - head) / V;
     int i = threadIdx.x;
-    for (; i + 3 * kBlock < vectors; i += 4 * kBlock) whole(std::integral_constant<int, 4>{}, head, i);
-    for (; i < vectors; i += kBlock) whole(std::integral_constant<int, 1>{}, head, i);
+    for (; i + 3 * kBlock < vectors; i += 4 * kBlock) four(std::true_type{}, head, i, vectors);
+    if (i < vectors) four(std::false_type{}, head, i, vectors);
     if (threadIdx.x < 2 * V) {
         const int j = (int)threadIdx.x < head ? (int)threadIdx.x : (int)threadIdx.x + vectors * V;
         if (j < n) single(j);
@@ -71,12 +71,15 @@ __device__ __forceinline__ double chunk_squares(const GradChunk& c) {
     double t = 0.0;
     over_chunk<V>(
         c.grad, 16 / V, c.n,
-        [&](auto count, int head, int i) {
-            constexpr int U = decltype(count)::value;
+        [&](auto whole, int head, int i, int vectors) {
+            constexpr int U = 4;
             const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const char*>(c.grad) + head * (16 / V)) + i;
             u32x4 w[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) w[u] = p[u * kBlock];
+            for (int u = 0; u < U; ++u) {
+                w[u] = u32x4{0, 0, 0, 0};
+                if (decltype(whole)::value || i + u * kBlock < vectors) w[u] = p[u * kBlock];
+            }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -127,15 +130,18 @@ __device__ __forceinline__ void chunk_scale(const GradChunk& c, float coef) {
     void* to = PACK ? static_cast<void*>(c.packed) : c.grad;
     over_chunk<4>(
         to, D, c.n,
-        [&](auto count, int head, int i) {
-            constexpr int U = decltype(count)::value;
+        [&](auto whole, int head, int i, int vectors) {
+            constexpr int U = 4;
             typedef std::conditional_t<BF16, u32x2_any, u32x4_any> Raw;
             typedef std::conditional_t<D == 2, u32x2r, u32x4> Out;
             const Raw* p = reinterpret_cast<const Raw*>(static_cast<const char*>(c.grad) + head * E) + i;
             Out* o = reinterpret_cast<Out*>(static_cast<char*>(to) + head * D) + i;
             Raw w[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) w[u] = __builtin_nontemporal_load(p + u * kBlock);
+            for (int u = 0; u < U; ++u) {
+                w[u] = Raw{};
+                if (decltype(whole)::value || i + u * kBlock < vectors) w[u] = __builtin_nontemporal_load(p + u * kBlock);
+            }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -155,7 +161,7 @@ __device__ __forceinline__ void chunk_scale(const GradChunk& c, float coef) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(v[j]);
                 }
-                __builtin_nontemporal_store(x, o + u * kBlock);
+                if (decltype(whole)::value || i + u * kBlock < vectors) __builtin_nontemporal_store(x, o + u * kBlock);
             }
         },
         [&](int j) { store_one<D == 2>(to, j, coef * load_one<BF16>(c.grad, j)); });

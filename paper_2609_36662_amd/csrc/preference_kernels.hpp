@@ -20,6 +20,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "matrix_view.hpp"
 
 namespace autoloco {
@@ -144,22 +146,25 @@ __device__ __forceinline__ RunningSum<PLAIN> row_sum(const char* x, int64_t voca
     const RowSplit<BF16> row(x, vocab);
     const u32x4* body = reinterpret_cast<const u32x4*>(x + row.head * (16 / V));
     RunningSum<PLAIN> r;
-    int64_t i = threadIdx.x;
-    for (; i + (U - 1) * NT < row.vectors; i += U * NT) {
+    // the last vectors of the row together too: one after another, each would wait for its
+    // own way to memory
+    constexpr uint32_t kNothing = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
+    auto batch = [&](int64_t i, auto whole) {
         u32x4 w[U];
         float v[U * V];
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = body[i + u * NT];
+        for (int u = 0; u < U; ++u) {
+            w[u] = u32x4{kNothing, kNothing, kNothing, kNothing};
+            if (decltype(whole)::value || i + u * NT < row.vectors) w[u] = body[i + u * NT];
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < U; ++u) unpack<BF16>(reinterpret_cast<float(&)[V]>(v[u * V]), w[u]);
         r.add(v);
-    }
-    for (; i < row.vectors; i += NT) {
-        float v[V];
-        unpack<BF16>(v, body[i]);
-        r.add(v);
-    }
+    };
+    int64_t i = threadIdx.x;
+    for (; i + (U - 1) * NT < row.vectors; i += U * NT) batch(i, std::true_type{});
+    if (i < row.vectors) batch(i, std::false_type{});
     if (threadIdx.x < 2 * V) {   // head and tail together: fewer than 2 V elements
         const int64_t j = row.single(threadIdx.x);
         if (j >= 0) {
@@ -297,7 +302,7 @@ __device__ __forceinline__ int64_t sequence_of(const SequenceArgs& a, int64_t ro
 template <bool BF16, int NT, bool PLAIN>
 __device__ __forceinline__ void row_gradient(const char* x, char* out, int64_t vocab, int64_t label, float w, float wp,
                                              float m) {
-    constexpr int U = 2;   // vectors in flight
+    constexpr int U = NT == 1024 ? 4 : 2;   // vectors in flight
     constexpr int V = BF16 ? 8 : 4;
     const RowSplit<BF16> row(out, vocab);
     const u32x4_any* in = reinterpret_cast<const u32x4_any*>(x + row.head * (16 / V));
@@ -323,16 +328,21 @@ __device__ __forceinline__ void row_gradient(const char* x, char* out, int64_t v
         }
         st_u4(&body[i], to);
     };
-    int64_t i = threadIdx.x;
-    for (; i + (U - 1) * NT < row.vectors; i += U * NT) {
+    auto batch = [&](int64_t i, auto whole) {
         u32x4 raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = __builtin_nontemporal_load(&in[i + u * NT]);
+        for (int u = 0; u < U; ++u) {
+            raw[u] = u32x4{0, 0, 0, 0};
+            if (decltype(whole)::value || i + u * NT < row.vectors) raw[u] = __builtin_nontemporal_load(&in[i + u * NT]);
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int u = 0; u < U; ++u) one(raw[u], i + u * NT);
-    }
-    for (; i < row.vectors; i += NT) one(in[i], i);
+        for (int u = 0; u < U; ++u)
+            if (decltype(whole)::value || i + u * NT < row.vectors) one(raw[u], i + u * NT);
+    };
+    int64_t i = threadIdx.x;
+    for (; i + (U - 1) * NT < row.vectors; i += U * NT) batch(i, std::true_type{});
+    if (i < row.vectors) batch(i, std::false_type{});
     if (threadIdx.x < 2 * V) {
         const int64_t j = row.single(threadIdx.x);
         if (j >= 0) {
