@@ -107,7 +107,7 @@ int autoloco_last_kernel_ms(autoloco_ctx* ctx, float* ms);
  * 4M parameters on, 12M with four or five payloads.  The reset: three, or fewer into
  * one or two replicas of large models and into nine bf16 or fourteen fp32 and more.
  * AdamW: two or three for the norms, one or two for the update.  Clipping over many
- * tensors: two, and at most 1,024 in all; the other operators of a local step have a
+ * tensors: two or three, and at most 1,024 in all; the other operators of a local step have a
  * workgroup a tile or a row, whatever the cap).  The round's statistics are bit-identical between runs with the
  * same n, k, replica type, device and cap, and between the standalone and the fused
  * call. */

@@ -14,6 +14,7 @@ using namespace autoloco;
 struct autoloco_grads {
     int device = 0;
     int32_t workers = 0;
+    int per_cu = 2;   // workgroups a compute unit, over all workers
     GradChunk* chunks = nullptr;
     int64_t first[AUTOLOCO_MAX_K + 1] = {};
 };
@@ -367,6 +368,10 @@ int autoloco_grads_create(autoloco_ctx* c, const autoloco_grad* t, int64_t count
         autoloco_grads list;
         list.device = c->device;
         list.workers = workers;
+        // Two workgroups a compute unit (two workers' 1.1B bf16 gradients 3.20 ms; 3.72 at one,
+        // 3.28 at three or four), three for lists of up to twice the small ones (10M bf16
+        // of one worker 19.0 us against 20.9, 18M of four 32.2 against 35.4).
+        list.per_cu = total <= 2 * kSmallList ? 3 : 2;
         const int64_t chunk = total <= kSmallList ? kSmallChunk : kChunk;
         std::vector<GradChunk> chunks;
         for (int32_t k = 0; k < workers; ++k) {
@@ -433,11 +438,9 @@ int autoloco_clip_grad_norm(autoloco_ctx* c, autoloco_grads* l, double max_norm,
         a.sums = c->sums;
         a.host_sums = c->host_sums_dev;
         a.norms = norms;
-        // two workgroups a compute unit over all workers (two workers' 1.1B bf16 gradients
-        // 3.20 ms; 3.72 at one, 3.28 at three or four)
         int64_t most = 1;
         for (int32_t k = 0; k < l->workers; ++k) most = std::max(most, l->first[k + 1] - l->first[k]);
-        const int64_t limit = std::max(1, (c->grid_limit > 0 ? std::min(c->grid_limit, 1024) : c->num_cus * 2) / l->workers);
+        const int64_t limit = std::max(1, (c->grid_limit > 0 ? std::min(c->grid_limit, 1024) : c->num_cus * l->per_cu) / l->workers);
         const int blocks = static_cast<int>(std::min(most, limit));
         st = launched(c, [&]() -> hipError_t {
             const hipError_t e = launch_tensor_norm(l->workers, blocks, a, c->stream);
