@@ -14,8 +14,9 @@ def row_logps(logits, labels):
         for r in range(rows):
             if 0 <= labels[r] < vocab:
                 top = np.max(x[r])
-                lse[r] = top + np.log(np.sum(np.exp(x[r] - top)))
-                lp[r] = x[r, labels[r]] - lse[r]
+                ln = np.log(np.sum(np.exp(x[r] - top)))
+                lse[r] = top + ln
+                lp[r] = (x[r, labels[r]] - top) - ln     # apart from top, which may be far larger
     return lp, lse
 
 
@@ -47,7 +48,7 @@ def preference(logits, labels, offsets, ref, beta, smoothing, scale):
         for s in range(seqs):
             for r in range(off[s], off[s + 1]):
                 if 0 <= labels[r] < vocab:
-                    grads[r] = -w[s] * np.exp(x[r] - lse[r])
+                    grads[r] = -w[s] * np.exp((x[r] - x[r, labels[r]]) + lp[r] if np.isfinite(lp[r]) else x[r] - lse[r])
                     grads[r, labels[r]] += w[s]
     return losses, logps, grads, w, lse
 

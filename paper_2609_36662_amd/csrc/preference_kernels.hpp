@@ -102,28 +102,36 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 constexpr float kLowest = -3.402823466e38f;
-// Beyond this magnitude x log2 e may overflow, and a row whose maximum lies there is
-// done again with differences first.
-constexpr float kHuge = 0x1p125f;
+// Up to this power of two an exponent x log2 e - m is as exact as its own size: m, itself a
+// rounded product, is taken as it is, so that nothing cancels but what the fused
+// multiply-add keeps.  A row whose maximum lies beyond is done again with differences first.
+constexpr float kHuge = 0x1p24f;
 
-// A running maximum and the sum of 2^((x - max) log2 e); PLAIN: the exponent is one
-// multiply-add of x, else the difference is taken first.
+// A running maximum and a sum of exponentials.  PLAIN: the maximum m is that of x log2 e,
+// rounded, the sum that of 2^(x log2 e - m), one multiply-add an exponent.  Else m is that
+// of x, the sum that of 2^((x - m) log2 e).
 template <bool PLAIN>
 struct RunningSum {
     float m = PLAIN ? -kHuge : kLowest, s = 0.f;   // values below the first m add nothing
     static __device__ __forceinline__ float power(float x, float m) {
         if constexpr (PLAIN)
-            return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -m * kLog2e));
+            return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -m));
         else
             return __builtin_amdgcn_exp2f((x - m) * kLog2e);
     }
+    // What a sum for maximum m is worth for maximum to.
+    static __device__ __forceinline__ float from(float m, float to) {
+        return __builtin_amdgcn_exp2f(PLAIN ? m - to : (m - to) * kLog2e);
+    }
     template <int N>
     __device__ __forceinline__ void add(const float (&x)[N]) {
-        float top = m;
+        float top = x[0];
 #pragma unroll
-        for (int i = 0; i + 1 < N; i += 2) top = max3(top, x[i], x[i + 1]);
-        if constexpr (N % 2 == 1) top = max3(top, x[N - 1], x[N - 1]);
-        s *= __builtin_amdgcn_exp2f((m - top) * kLog2e);
+        for (int i = 1; i + 1 < N; i += 2) top = max3(top, x[i], x[i + 1]);
+        if constexpr (N % 2 == 0) top = max3(top, x[N - 1], x[N - 1]);
+        if constexpr (PLAIN) top *= kLog2e;
+        top = max3(m, top, top);
+        s *= from(m, top);
         m = top;
         float part[2] = {0.f, 0.f};
 #pragma unroll
@@ -132,7 +140,7 @@ struct RunningSum {
     }
     __device__ __forceinline__ void join(float om, float os) {
         const float to = max3(m, om, om);
-        s = s * __builtin_amdgcn_exp2f((m - to) * kLog2e) + os * __builtin_amdgcn_exp2f((om - to) * kLog2e);
+        s = s * from(m, to) + os * from(om, to);
         m = to;
     }
 };
@@ -204,15 +212,22 @@ __global__ void __launch_bounds__(NT) row_logp_kernel(SequenceArgs a, int64_t fi
     }
     const char* x = static_cast<const char*>(a.logits.data) + row * a.logits.stride * (BF16 ? 2 : 4);
     const RunningSum<true> r = row_sum<BF16, NT, true>(x, a.logits.cols, lds);
-    double m = r.m, s = r.s;
-    if (fabsf(r.m) >= kHuge) {   // every thread has the same maximum
-        __syncthreads();
-        const RunningSum<false> d = row_sum<BF16, NT, false>(x, a.logits.cols, lds);
-        m = d.m;
-        s = d.s;
+    if (fabsf(r.m) < kHuge) {   // every thread has the same maximum
+        if (threadIdx.x == 0) {
+            const float at = load_one<BF16>(x, label);
+            const double sum = log2((double)r.s);
+            a.lse[row] = (float)((r.m + sum) / kLog2e);
+            // a large probability with the same rounding as in the sum, so that it is at most 1
+            const float power = __builtin_fmaf(at, kLog2e, -r.m);
+            const double part = power > -1.f ? log2((double)__builtin_amdgcn_exp2f(power)) : (double)at * kLog2e - r.m;
+            a.logp[row] = (float)((part - sum) / kLog2e);
+        }
+        return;
     }
+    __syncthreads();
+    const RunningSum<false> d = row_sum<BF16, NT, false>(x, a.logits.cols, lds);
     if (threadIdx.x == 0) {
-        const double ln = log(s);   // apart from m, which may be far larger
+        const double m = d.m, ln = log((double)d.s);   // apart from m, which may be far larger
         a.lse[row] = (float)(m + ln);
         a.logp[row] = (float)(((double)load_one<BF16>(x, label) - m) - ln);
     }
@@ -295,24 +310,28 @@ __device__ __forceinline__ int64_t sequence_of(const SequenceArgs& a, int64_t ro
     return lo;
 }
 
-// One row of the gradient: -wp exp(x - m), and w more at the label.  Neither the logits
+// One row of the gradient: -wp times the power of RunningSum (PLAIN: with what rounding
+// took from m given back, so that a probability of 1 is 1), and w more at the label.  Neither the logits
 // nor the gradient are kept in the caches: both pass once (18,500 rows of 32,000 bf16:
 // 511 us for the whole call against 541 with cached loads and 558 with cached stores
 // too; 3,900 rows of fp32 199, 236 and 256).
 template <bool BF16, int NT, bool PLAIN>
 __device__ __forceinline__ void row_gradient(const char* x, char* out, int64_t vocab, int64_t label, float w, float wp,
-                                             float m) {
+                                             float m, float rest) {
     constexpr int U = NT == 1024 ? 4 : 2;   // vectors in flight
     constexpr int V = BF16 ? 8 : 4;
     const RowSplit<BF16> row(out, vocab);
     const u32x4_any* in = reinterpret_cast<const u32x4_any*>(x + row.head * (16 / V));
     u32x4* body = reinterpret_cast<u32x4*>(out + row.head * (16 / V));
     const int64_t at = label - row.head;
+    auto power = [&](float e) {
+        return PLAIN ? __builtin_amdgcn_exp2f(__builtin_fmaf(e, kLog2e, -m) + rest) : RunningSum<false>::power(e, m);
+    };
     auto one = [&](u32x4 raw, int64_t i) {
         float v[V];
         unpack<BF16>(v, raw);
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = -wp * RunningSum<PLAIN>::power(v[j], m);
+        for (int j = 0; j < V; ++j) v[j] = -wp * power(v[j]);
         if ((uint64_t)(at - i * V) < (uint64_t)V) {
 #pragma unroll
             for (int j = 0; j < V; ++j)
@@ -346,7 +365,7 @@ __device__ __forceinline__ void row_gradient(const char* x, char* out, int64_t v
     if (threadIdx.x < 2 * V) {
         const int64_t j = row.single(threadIdx.x);
         if (j >= 0) {
-            float v = -wp * RunningSum<PLAIN>::power(load_one<BF16>(x, j), m);
+            float v = -wp * power(load_one<BF16>(x, j));
             if (j == label) v += w;
             store_one<BF16>(out, j, v);
         }
@@ -380,6 +399,19 @@ __global__ void __launch_bounds__(NT) logit_grad_kernel(SequenceArgs a, Preferen
         }
         return;
     }
+    const char* x = static_cast<const char*>(a.logits.data) + row * a.logits.stride * (BF16 ? 2 : 4);
+    // The row's log sum exp: as stored, or the label's logit less its log-probability,
+    // whichever is the smaller number and so the more exact.  Taken before the barrier: the
+    // gradient may go where the logits are.
+    // Where both numbers are beyond 64, or the exponent is beyond 2^24, the sum is done again.
+    __shared__ float norm[2];
+    if (threadIdx.x == 0) {
+        const float lse = a.lse[row], logp = a.logp[row];
+        const double exponent = (fabsf(logp) < fabsf(lse) ? (double)load_one<BF16>(x, label) - logp : (double)lse) * kLog2e;
+        const bool exact = fminf(fabsf(lse), fabsf(logp)) < 64.f && fabs(exponent) < kHuge;
+        norm[0] = exact ? (float)exponent : kHuge;
+        norm[1] = (float)(norm[0] - exponent);
+    }
     const int64_t s = sequence_of(a, row), half = a.sequences / 2;
     float w;
     if constexpr (PAIRS) {
@@ -388,15 +420,14 @@ __global__ void __launch_bounds__(NT) logit_grad_kernel(SequenceArgs a, Preferen
         w = (float)(s < half ? chosen : -chosen);
     } else {
         w = a.weight[s];
+        __syncthreads();
     }
-    const char* x = static_cast<const char*>(a.logits.data) + row * a.logits.stride * (BF16 ? 2 : 4);
-    const float lse = a.lse[row];
-    if (fabsf(lse) < kHuge) {
-        row_gradient<BF16, NT, true>(x, out, vocab, label, w, w, lse);
+    if (norm[0] < kHuge) {
+        row_gradient<BF16, NT, true>(x, out, vocab, label, w, w, norm[0], norm[1]);
     } else {   // the maximum and the sum apart (and a NaN)
         __shared__ float sums[2 * (NT / 64)];
         const RunningSum<false> r = row_sum<BF16, NT, false>(x, vocab, sums);
-        row_gradient<BF16, NT, false>(x, out, vocab, label, w, w / r.s, r.m);
+        row_gradient<BF16, NT, false>(x, out, vocab, label, w, w / r.s, r.m, 0.f);
     }
 }
 

@@ -348,3 +348,57 @@ def test_refusals(ctx):
     with pytest.raises(ValueError):
         al.make_sequences(x, labels, off, f(15))
 
+
+
+def _check_shifted(x, labels, off, ref, got, beta, dtype):
+    """As _check, with tolerances that do not grow with what a row's logits have in common.
+
+    An exponential's exponent is rounded by 2^-24 of its own size, which, weighted by the
+    probabilities, is at most 2^-24 (ln V + 1) for the whole sum, and the instruction by 2^-23.  The gradient
+    takes the normaliser from numbers of at most 64 rounded to fp32, or adds it up again."""
+    x, labels, off = x.double().cpu().numpy(), labels.numpy(), off.numpy()
+    losses, logps, g, w, lse = opref.preference(x, labels, off, ref.numpy(), beta, 0.0, 1.0)
+    lp, _ = opref.row_logps(x, labels)
+    vocab, p = x.shape[1], len(losses)
+    e = (8 * -(-vocab // 2048) + 16) * 2.0 ** -24 + 2.0 ** -22 * (np.log(vocab) + 2)
+    row_tol = np.where((labels >= 0) & (labels < vocab), e + 2.0 ** -22 * np.abs(lp), 0.0)
+    seq_tol = np.array([row_tol[a:b].sum() for a, b in zip(off, off[1:])])
+    work = got[2].double().cpu().numpy()
+    rows = len(labels)
+    assert np.all(np.abs(work[rows:2 * rows] - lp) <= row_tol), np.abs(work[rows:2 * rows] - lp).max()
+    assert np.all(work[rows:2 * rows] <= 0)
+    np.testing.assert_array_less(np.abs(got[1].double().cpu().numpy() - logps), seq_tol + 2.0 ** -24 * np.abs(logps) + 1e-30)
+    z_tol = abs(beta) * (seq_tol[:p] + seq_tol[p:])
+    np.testing.assert_array_less(np.abs(got[0].double().cpu().numpy() - losses), z_tol + 2.0 ** -23 * np.abs(losses) + 1e-30)
+    w_tol = np.concatenate([abs(beta) * z_tol / 4] * 2) + 2.0 ** -23 * np.abs(w)
+    out = 2.0 ** -23 if dtype == "f32" else 2.0 ** -8
+    gg = got[3].double().cpu().numpy()
+    for s in range(len(logps)):
+        for r in range(off[s], off[s + 1]):
+            if not 0 <= labels[r] < vocab:
+                assert not gg[r].any()
+                continue
+            d = (x[r] - x[r, labels[r]]) + lp[r]
+            prob = np.exp(d)
+            rel = 2 * e + 2.0 ** -22 * (np.abs(d) + min(abs(lse[r]), abs(lp[r]), 64.0) + 2)
+            tol = abs(w[s]) * (prob * rel + 2.0 ** -23 * (np.arange(vocab) == labels[r])) + w_tol[s] + out * np.abs(g[r]) + 1e-38
+            assert np.all(np.abs(gg[r] - g[r]) <= tol), (r, np.abs(gg[r] - g[r]).max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [5, 301, 2051, 8209])
+@pytest.mark.parametrize("shift", [100.0, -3000.0, 5e4, -1.1e7, 1.3e7, -1e9, 3e10, -1e20, 2e37])
+def test_what_all_logits_of_a_row_have_in_common(ctx, shift, vocab, dtype):
+    """A shift of all of a row's logits changes neither probabilities nor gradients, however large (also a whole row
+    of an additive mask's -1e9); a label far below the rest of such a row has its log-probability."""
+    x, labels, off, ref = _inputs([3, 4, 5, 2], vocab, dtype, 31, mask=0.0)
+    x = (x.float() + shift).to(DT[dtype])
+    x[0] = shift                                       # nothing but the shift
+    x[4, int(labels[4])] = shift - 1000.0              # an improbable label
+    x[9, int(labels[9])] = shift + 30.0                # a nearly certain one
+    labels[6] = -1
+    ref = torch.from_numpy(np.add.reduceat(opref.row_logps(x.double().numpy(), labels.numpy())[0], off.numpy()[:-1]).astype(np.float32))
+    got = _run(ctx, x, labels, off, ref)
+    _check_shifted(x, labels, off, ref, got, 0.1, dtype)
+    there = _run(ctx, x.cuda(), labels, off, ref, grads="in place")
+    assert torch.equal(there[3], got[3])
