@@ -5,7 +5,7 @@
 //
 // The tensors are cut into chunks of at most kChunk elements, listed worker by
 // worker in a table in device memory.  Two streaming passes over the chunks, one
-// grid row a worker: the squares (fp32 per 8 values, fp64 beyond, the reductions of
+// grid row a worker: the squares (in fp64, which costs nothing beside the reading, the reductions of
 // reduce.hpp), then the scaling, in which every workgroup adds its worker's sums up
 // again as the AdamW step does, so that no kernel stands between the passes.  Bound by
 // HBM: the gradients are read twice and written once.  Two workers' 1.1B bf16 gradients
@@ -69,6 +69,7 @@ template <bool BF16>
 __device__ __forceinline__ double chunk_squares(const GradChunk& c) {
     constexpr int V = BF16 ? 8 : 4;
     double t = 0.0;
+    auto add = [&](float g) { t = __builtin_fma((double)g, (double)g, t); };
     over_chunk<V>(
         c.grad, 16 / V, c.n,
         [&](auto whole, int head, int i, int vectors) {
@@ -83,23 +84,18 @@ __device__ __forceinline__ double chunk_squares(const GradChunk& c) {
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                float s = 0.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if constexpr (BF16) {
-                        s = __builtin_fmaf(bf16_lo(w[u][j]), bf16_lo(w[u][j]), s);
-                        s = __builtin_fmaf(bf16_hi(w[u][j]), bf16_hi(w[u][j]), s);
+                        add(bf16_lo(w[u][j]));
+                        add(bf16_hi(w[u][j]));
                     } else {
-                        s = __builtin_fmaf(__uint_as_float(w[u][j]), __uint_as_float(w[u][j]), s);
+                        add(__uint_as_float(w[u][j]));
                     }
                 }
-                t += (double)s;
             }
         },
-        [&](int j) {
-            const float g = load_one<BF16>(c.grad, j);
-            t += (double)(g * g);
-        });
+        [&](int j) { add(load_one<BF16>(c.grad, j)); });
     return t;
 }
 

@@ -220,3 +220,19 @@ def test_refusals(ctx):
     with pytest.raises(err):
         al.autoloco_clip_grad_norm(ctx, lst, 1.0)
     al.autoloco_grads_destroy(lst)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [2.0 ** 100, 2.0 ** -100])
+def test_squares_beyond_the_range_of_fp32(ctx, size, dtype):
+    """Gradients whose squares neither overflow nor vanish: norms and clipped values as for any other."""
+    g = torch.Generator().manual_seed(3)
+    ts = [(torch.randn(n, generator=g) * size).to(DT[dtype]).cuda() for n in (5001, 3, 70001)]
+    norm, c, want = opref.clip([[t.double().cpu().numpy() for t in ts]], size)[0]
+    packed = torch.empty(sum(t.numel() for t in ts), device="cuda")
+    norms = torch.empty(1, device="cuda")
+    st = al.autoloco_clip_grad_norm(ctx, al.autoloco_grads_create(ctx, [ts], [packed]), size, norms=norms)
+    assert abs(st.grad_norm[0] - norm) <= 4 * 2.0 ** -24 * norm and abs(float(norms[0]) - norm) <= 5 * 2.0 ** -24 * norm
+    assert abs(st.clip_coef[0] - c) <= 5 * 2.0 ** -24 * c and st.finite
+    ref = np.concatenate(want)
+    assert np.all(np.abs(packed.double().cpu().numpy() - ref) <= 8 * 2.0 ** -24 * np.abs(ref) + 2.0 ** -149)
