@@ -488,7 +488,8 @@ int autoloco_adamw_traffic_reference(autoloco_ctx* ctx, const autoloco_adamw_buf
 /* rows x cols elements of dtype (autoloco_dtype), row r at data + r * stride
  * elements.  stride >= cols for an output of more than one row; an input may
  * have any stride >= 0 (0: the same row again and again).
- * rows, cols in 0..2^30, stride in 0..2^40. */
+ * rows, cols in 0..2^30, stride in 0..2^40, from the first element to the last
+ * at most 2^48. */
 typedef struct {
     void* data;
     int64_t rows, cols, stride;

@@ -23,6 +23,7 @@ namespace {
 
 constexpr int64_t kMaxDim = int64_t(1) << 30;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
+constexpr int64_t kMaxSpan = int64_t(1) << 48;   // elements from a matrix's first to its last
 
 // Columns of a product: a tile's rows lie within 32 bits of its first.
 constexpr int64_t kMaxProductCols = int64_t(1) << 24;
@@ -82,7 +83,8 @@ struct Buffers {
 int check_matrix(autoloco_ctx* c, const autoloco_matrix& m, const char* name, bool written) {
     if (m.dtype != AUTOLOCO_F32 && m.dtype != AUTOLOCO_BF16)
         return fail(c, AUTOLOCO_E_INVALID, std::string("unknown dtype of ") + name);
-    if (m.rows < 0 || m.rows > kMaxDim || m.cols < 0 || m.cols > kMaxDim || m.stride < 0 || m.stride > kMaxStride)
+    if (m.rows < 0 || m.rows > kMaxDim || m.cols < 0 || m.cols > kMaxDim || m.stride < 0 || m.stride > kMaxStride ||
+        (m.rows > 1 && m.stride > (kMaxSpan - m.cols) / (m.rows - 1)))
         return fail(c, AUTOLOCO_E_INVALID, std::string("shape of ") + name + " out of range");
     if (written && m.rows > 1 && m.stride < m.cols)
         return fail(c, AUTOLOCO_E_INVALID, std::string("rows of ") + name + " overlap");

@@ -388,3 +388,16 @@ def test_graph_replays(ctx):
             work()
             stream.synchronize()
             assert torch.equal(got[0], y) and torch.equal(got[1], y1)
+
+
+@pytest.mark.parametrize("rows,stride", [(1 << 30, 1 << 40), ((1 << 24) + 1, 1 << 40), (1 << 30, 1 << 19)])
+def test_a_matrix_longer_than_any_memory_is_refused(ctx, rows, stride):
+    """Rows and strides in range whose product is not: the span must not wrap round 64 bits."""
+    x = torch.zeros((4, 64), device="cuda")
+    q = al.Mxfp4.empty(4, 64)
+    m = al._lib.Matrix(x.data_ptr(), rows, 4, stride, 0)
+    lib, handle = al.lib(), ctx.handle
+    assert lib.autoloco_mxfp4_quantize(handle, C.byref(m), C.byref(q.buffers), None) == -1
+    assert "shape of x out of range" in al.autoloco_last_error(ctx)
+    assert lib.autoloco_mxfp4_dequantize(handle, C.byref(q.buffers), C.byref(m)) == -1
+    assert "shape of out out of range" in al.autoloco_last_error(ctx)
