@@ -402,3 +402,32 @@ def test_what_all_logits_of_a_row_have_in_common(ctx, shift, vocab, dtype):
     _check_shifted(x, labels, off, ref, got, 0.1, dtype)
     there = _run(ctx, x.cuda(), labels, off, ref, grads="in place")
     assert torch.equal(there[3], got[3])
+
+
+@pytest.mark.parametrize("lens", [[5, 3, 0, 7], [700, 600, 650, 630]], ids=["pairs in the gradient's kernel", "pairs apart"])
+def test_graph_replays(lens):
+    """Captured into a graph and replayed on new logits, with eager work between, every replay gives the eager result."""
+    x, labels, off, ref = _inputs(lens, 200, "f32", 17)
+    stream = torch.cuda.Stream()
+    with al.autoloco_create(0, stream) as c, torch.cuda.stream(stream):
+        d = [t.cuda() for t in (x, labels, off, ref)]
+        losses, logps = torch.zeros(2, device="cuda"), torch.zeros(4, device="cuda")
+        work, g = torch.zeros(2 * sum(lens) + 4, device="cuda"), torch.zeros_like(d[0])
+
+        def call():
+            al.autoloco_preference_loss(c, *d, losses, logps, work, grads=g, label_smoothing=0.1)
+
+        call()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call()
+        for turn in range(3):
+            d[0].copy_(x * (turn + 1))
+            call()
+            want = [t.clone() for t in (losses, logps, g)]
+            for t in (losses, logps, work, g):
+                t.fill_(9.0)
+            graph.replay()
+            stream.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, (losses, logps, g)))
