@@ -22,10 +22,12 @@ hipError_t in_slices(int64_t blocks, Launch launch) {
 
 template <bool BF16>
 hipError_t quantize(const MatrixView& x, const Mx4* q, const Mx4* qt, hipStream_t s) {
-    if (qt == nullptr)
-        return in_slices(group_blocks(*q), [&](uint32_t first, dim3 grid) {
-            hipLaunchKernelGGL(mx_rows_kernel<BF16>, grid, dim3(kBlock), 0, s, x, *q, first);
+    if (qt == nullptr) {
+        const uint32_t nt = (uint32_t)((q->groups + kRowsGroups - 1) / kRowsGroups);
+        return in_slices(nt * ((q->rows + 15) / 16), [&](uint32_t first, dim3 grid) {
+            hipLaunchKernelGGL(mx_rows_kernel<BF16>, grid, dim3(kBlock), 0, s, x, *q, nt, first);
         });
+    }
     // whole groups of 128 columns, so that the padding is written too
     const uint32_t tiles = (uint32_t)((x.cols + 127) / 128) * (BF16 ? 1 : 2);
     return in_slices(tiles * ((x.rows + 127) / 128), [&](uint32_t first, dim3 grid) {

@@ -164,24 +164,46 @@ __device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
 }
 
 // ---------------------------------------------------------------- quantise --
-// Along the rows: a lane takes 8 columns, four lanes a block.  Bound by reading x.
-// first: the launch's first workgroup (a grid has fewer than 2^32 threads).
+// Along the rows: a lane takes 8 columns of each of U neighbouring groups, four lanes a
+// block; a workgroup 16 rows (nt workgroups across; first: the launch's first one, since a
+// grid has fewer than 2^32 threads).  Bound by reading x and, with bf16, still by the
+// instructions: two groups an address, where one for each, found by dividing a thread's
+// number, took 22.8 us for 20,000 x 2,048 bf16 against 19.2 (5.4 TB/s) and 15.5 against 14.6
+// for 4,096 x 4,096 fp32; four groups 20.4 and 16.0.
+constexpr int kRowsGroups = 2;
 template <bool BF16>
-__global__ void __launch_bounds__(kBlock) mx_rows_kernel(MatrixView x, Mx4 q, uint32_t first) {
-    const int64_t t = ((int64_t)first + blockIdx.x) * kBlock + threadIdx.x;
-    const uint32_t unit = (uint32_t)(t >> 4);   // 128 columns of a row
-    const uint32_t row = unit / (uint32_t)q.groups, group = unit % (uint32_t)q.groups;
-    if (row >= q.rows) return;
-    const int piece = t & 15;
-    uint32_t v[kWords8<BF16>];
-    load_raw<BF16>(v, static_cast<const char*>(x.data) + (int64_t)row * x.stride * (BF16 ? 2 : 4),
-                   (int64_t)group * 128 + piece * 8, x.cols);
-    uint32_t m = mx_amax<BF16>(v);
-    m = max_dpp<0xB1>(m);   // lanes ^ 1, then ^ 2: the block's four
-    m = max_dpp<0x4E>(m);
-    const uint32_t s = mx_scale(m);
-    *reinterpret_cast<uint32_t*>(q.codes + (int64_t)row * q.row_bytes + group * 64 + piece * 4) = mx_codes8_raw<BF16>(v, s);
-    if ((piece & 3) == 0) q.scales[((int64_t)group * q.rows + row) * 4 + (piece >> 2)] = (uint8_t)s;
+__global__ void __launch_bounds__(kBlock) mx_rows_kernel(MatrixView x, Mx4 q, uint32_t nt, uint32_t first) {
+    constexpr int U = kRowsGroups;
+    const uint32_t b = first + blockIdx.x, rt = b / nt;
+    const int g0 = (int)(b % nt) * U;
+    const int piece = threadIdx.x & 15;
+    const int64_t row = (int64_t)rt * 16 + (threadIdx.x >> 4);
+    const bool there = row < q.rows;
+    const char* from = static_cast<const char*>(x.data) + (there ? row : q.rows - 1) * x.stride * (BF16 ? 2 : 4);
+    const int64_t c0 = (int64_t)g0 * 128 + piece * 8;
+    uint32_t v[U][kWords8<BF16>];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if ((int64_t)(g0 + u + 1) * 128 <= x.cols)   // the same in every lane
+            load_raw<BF16>(v[u], from + c0 * (BF16 ? 2 : 4), u * 128, u * 128 + 8);
+        else
+            load_raw<BF16>(v[u], from, c0 + u * 128, x.cols);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    uint8_t* codes = q.codes + row * q.row_bytes + g0 * 64 + piece * 4;
+    uint8_t* scales = q.scales + ((int64_t)g0 * q.rows + row) * 4 + (piece >> 2);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        uint32_t m = mx_amax<BF16>(v[u]);
+        m = max_dpp<0xB1>(m);   // lanes ^ 1, then ^ 2: the block's four
+        m = max_dpp<0x4E>(m);
+        const uint32_t s = mx_scale(m);
+        const uint32_t w = mx_codes8_raw<BF16>(v[u], s);
+        if (there && g0 + u < q.groups) {
+            *reinterpret_cast<uint32_t*>(codes + u * 64) = w;
+            if ((piece & 3) == 0) scales[u * q.rows * 4] = (uint8_t)s;
+        }
+    }
 }
 
 // Along the columns (and the rows): a workgroup takes 128 rows of 256 bytes, all loads
