@@ -38,55 +38,4 @@ __device__ __forceinline__ void store_one(void* p, int64_t i, float v) {
         static_cast<float*>(p)[i] = v;
 }
 
-// Elements i..i+7 of a row of n (those past n: fill).
-template <bool BF16>
-__device__ __forceinline__ void load8(float (&x)[8], const void* row, int64_t i, int64_t n, float fill = 0.f) {
-    if (i + 8 <= n) {
-        if constexpr (BF16) {
-            const u32x4_any w = *reinterpret_cast<const u32x4_any*>(static_cast<const uint16_t*>(row) + i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[2 * j] = bf16_lo(w[j]);
-                x[2 * j + 1] = bf16_hi(w[j]);
-            }
-        } else {
-            const u32x4_any* p = reinterpret_cast<const u32x4_any*>(static_cast<const float*>(row) + i);
-            const u32x4_any a = p[0], b = p[1];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[j] = __uint_as_float(a[j]);
-                x[4 + j] = __uint_as_float(b[j]);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = i + j < n ? load_one<BF16>(row, i + j) : fill;
-    }
-}
-template <bool BF16>
-__device__ __forceinline__ void store8(void* row, int64_t i, int64_t n, const float (&x)[8]) {
-    if (i + 8 <= n) {
-        if constexpr (BF16) {
-            u32x4_any w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = bf16_pack(x[2 * j], x[2 * j + 1]);
-            *reinterpret_cast<u32x4_any*>(static_cast<uint16_t*>(row) + i) = w;
-        } else {
-            u32x4_any* p = reinterpret_cast<u32x4_any*>(static_cast<float*>(row) + i);
-            u32x4_any a, b;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                a[j] = __float_as_uint(x[j]);
-                b[j] = __float_as_uint(x[4 + j]);
-            }
-            p[0] = a;
-            p[1] = b;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (i + j < n) store_one<BF16>(row, i + j, x[j]);
-    }
-}
-
 }  // namespace autoloco

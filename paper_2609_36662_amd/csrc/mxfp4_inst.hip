@@ -5,9 +5,6 @@ namespace autoloco {
 
 namespace {
 
-// Workgroups of kBlock threads, 16 of them a row's 128 columns.
-int64_t group_blocks(const Mx4& q) { return (q.rows * q.groups * 16 + kBlock - 1) / kBlock; }
-
 // launch(first, count) over all workgroups, at most 2^20 at a time.
 template <typename Launch>
 hipError_t in_slices(int64_t blocks, Launch launch) {
@@ -35,6 +32,14 @@ hipError_t quantize(const MatrixView& x, const Mx4* q, const Mx4* qt, hipStream_
             hipLaunchKernelGGL((mx_cols_kernel<BF16, true>), grid, dim3(kBlock), 0, s, x, *q, *qt, tiles, first);
         else
             hipLaunchKernelGGL((mx_cols_kernel<BF16, false>), grid, dim3(kBlock), 0, s, x, *qt, *qt, tiles, first);
+    });
+}
+
+template <bool BF16>
+hipError_t values(const Mx4& q, const MatrixOut& out, hipStream_t s) {
+    const uint32_t nt = (uint32_t)((q.groups + kRowsGroups - 1) / kRowsGroups);
+    return in_slices(nt * ((q.rows + kValueRows<BF16> - 1) / kValueRows<BF16>), [&](uint32_t first, dim3 grid) {
+        hipLaunchKernelGGL(mx_values_kernel<BF16>, grid, dim3(kBlock), 0, s, q, out, nt, first);
     });
 }
 
@@ -114,12 +119,7 @@ hipError_t launch_mx_quantize(bool bf16, const MatrixView& x, const Mx4* q, cons
 }
 
 hipError_t launch_mx_values(bool bf16, const Mx4& q, const MatrixOut& out, hipStream_t s) {
-    return in_slices(group_blocks(q), [&](uint32_t first, dim3 grid) {
-        if (bf16)
-            hipLaunchKernelGGL(mx_values_kernel<true>, grid, dim3(kBlock), 0, s, q, out, first);
-        else
-            hipLaunchKernelGGL(mx_values_kernel<false>, grid, dim3(kBlock), 0, s, q, out, first);
-    });
+    return bf16 ? values<true>(q, out, s) : values<false>(q, out, s);
 }
 
 hipError_t launch_mx_matmul(bool bf16, const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t s) {
