@@ -330,8 +330,10 @@ __global__ void __launch_bounds__(kBlock) mx_cols_kernel(MatrixView x, Mx4 q, Mx
 // -------------------------------------------------------------- dequantise --
 // A lane writes 16 bytes of each of two neighbouring groups, so that neighbouring lanes
 // write neighbouring ones; a workgroup 16 rows (bf16) or 8, nt workgroups across.  Bound by
-// writing, past the caches (50,257 x 768 fp32 26.5 us, 6.6 TB/s, against 34.3 through them;
-// with 32 bytes a lane and values put together from bits 46.9).
+// writing (50,257 x 768 fp32 34 us, 5.1 TB/s; with 32 bytes a lane and values put together
+// from bits 47).  Stores past the caches take 27 us, but whoever reads the values next
+// pays for it: 8,192 x 4,096 fp32 with its 4-bit form taken again 50 and 53 us, multiplied in
+// place 76 against 71; 4,096 x 4,096 26.8 against 25.7 and 35.4 against 33.5.
 template <bool BF16>
 constexpr int kValueRows = BF16 ? 16 : 8;
 template <bool BF16>
@@ -364,7 +366,7 @@ __global__ void __launch_bounds__(kBlock) mx_values_kernel(Mx4 q, MatrixOut out,
         const int64_t c = (int64_t)(g0 + u) * 128 + piece * V;
         const u32x4 v = mx_values_raw<BF16>(w[u], s[u]);
         if (c + V <= out.cols) {
-            __builtin_nontemporal_store(u32x4_any(v), reinterpret_cast<u32x4_any*>(to + c * (BF16 ? 2 : 4)));
+            *reinterpret_cast<u32x4_any*>(to + c * (BF16 ? 2 : 4)) = v;
         } else {
 #pragma unroll
             for (int e = 0; e < V; ++e)
