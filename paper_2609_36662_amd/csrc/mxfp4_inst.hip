@@ -101,9 +101,9 @@ hipError_t matmul(const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t 
 // workgroup.
 template <bool BF16, int R, int NW>
 hipError_t tokens_at(const MatrixView& x, const Mx4& w, const MatrixOut& y, hipStream_t s) {
-    const unsigned blocks = (unsigned)((w.rows + 16 * R - 1) / (16 * R));
-    hipLaunchKernelGGL((mx_tokens_kernel<BF16, R, NW>), dim3(blocks), dim3(NW * 64), 0, s, x, w, y);
-    return hipGetLastError();
+    return in_slices((w.rows + 16 * R - 1) / (16 * R), [&](uint32_t first, dim3 grid) {
+        hipLaunchKernelGGL((mx_tokens_kernel<BF16, R, NW>), grid, dim3(NW * 64), 0, s, x, w, y, first);
+    });
 }
 template <bool BF16>
 hipError_t tokens(const MatrixView& x, const Mx4& w, const MatrixOut& y, hipStream_t s) {

@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kBlock) mx_values_kernel(Mx4 q, MatrixOut out,
 __device__ __forceinline__ i32x8 operand(u32x4 w) { return i32x8{(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0}; }
 
 // Up to 16 rows of x, quantised as they are read.  A workgroup takes 16 R rows of the
-// weight; its NW waves take groups of 128 columns in turn and are joined in LDS in wave
+// weight (first: the launch's first one); its NW waves take groups of 128 columns in turn and are joined in LDS in wave
 // order.  A wave reads x in whole rows, 8 columns a lane and four rows at a time,
 // quantises them as mx_rows_kernel does, and passes the codes through its own piece of
 // LDS into the order of the 16x16x128 instruction: row lane % 16, columns 32 (lane / 16)
@@ -394,14 +394,14 @@ __device__ __forceinline__ i32x8 operand(u32x4 w) { return i32x8{(int)w[0], (int
 // latency of the weight's and x's loads, then by the quantisation (one row of x 7.4 us
 // where thirteen take 9.6): 24 MB of weight at 2.5 TB/s, launch included.
 template <bool BF16, int R, int NW>
-__global__ void __launch_bounds__(NW * 64) mx_tokens_kernel(MatrixView x, Mx4 w, MatrixOut y) {
+__global__ void __launch_bounds__(NW * 64) mx_tokens_kernel(MatrixView x, Mx4 w, MatrixOut y, uint32_t first) {
     constexpr int W = kWords8<BF16>;
     constexpr int kRow = 80;                       // bytes of a row of codes: 16 rows' pieces in 64 banks
     __shared__ __align__(16) uint8_t xlds[NW][16 * kRow + 64];
     __shared__ float part[NW][R * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, j = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * (16 * R);
+    const int64_t n0 = ((int64_t)first + blockIdx.x) * (16 * R);
     const uint8_t* wc[R];
     const uint8_t* ws[R];
 #pragma unroll
