@@ -182,8 +182,10 @@ __global__ void __launch_bounds__(256, T == 1 || (T == 2 && ST == 2) ? 2 : 1) mx
     Scales sc[2];
     int i = 0;
     auto reading = [&](int at, auto phase_of) {
-        constexpr int s = decltype(phase_of)::value;
-        return [&, at](auto j) { read(f[s % (2 * D)], sc[s / 2], at, s, j); };
+        return [&, at](auto j) {
+            constexpr int s = decltype(phase_of)::value;
+            read(f[s % (2 * D)], sc[s / 2], at, s, j);
+        };
     };
     // Phase s of step i; it reads the operands of phase s + D (next: also those of the
     // next step) and issues the loads x.
