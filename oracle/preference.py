@@ -42,7 +42,8 @@ def preference(logits, labels, offsets, ref, beta, smoothing, scale):
             losses = losses - (1 - smoothing) * log_sigmoid(z)
         if smoothing > 0:
             losses = losses - smoothing * log_sigmoid(-z)
-        w = scale * beta * (1 / (1 + np.exp(-z)) - (1 - smoothing))
+        # sigma(z) - (1 - smoothing), without its cancellation where sigma(z) is close to 1
+        w = scale * beta * (smoothing / (1 + np.exp(-z)) - (1 - smoothing) / (1 + np.exp(z)))
         w = np.concatenate([w, -w])
         grads = np.zeros((rows, vocab))
         for s in range(seqs):

@@ -260,7 +260,11 @@ __device__ __forceinline__ double pair_weight(const SequenceArgs& a, const Prefe
     first = sum_rows<NT>(a.logp, offset_at(a, i), offset_at(a, i + 1), lds);
     second = sum_rows<NT>(a.logp, offset_at(a, j), offset_at(a, j + 1), lds);
     z = p.beta * ((first - (double)p.ref[i]) - (second - (double)p.ref[j]));
-    return p.scale * p.beta * (1.0 / (1.0 + exp(-z)) - (1.0 - p.smoothing));
+    // sigma(z) - (1 - eps) = eps sigma(z) - (1 - eps) sigma(-z): where the pair is decided,
+    // the difference on the left keeps nothing of a weight of exp(-z)
+    const double e = exp(-fabs(z)), larger = 1.0 / (1.0 + e), smaller = e * larger;
+    const double up = z < 0.0 ? smaller : larger, down = z < 0.0 ? larger : smaller;
+    return p.scale * p.beta * (p.smoothing * up - (1.0 - p.smoothing) * down);
 }
 
 // What a workgroup of NT threads writes for pair i (or, without losses, sequence i).
