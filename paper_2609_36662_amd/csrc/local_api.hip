@@ -320,13 +320,19 @@ int autoloco_preference_loss(autoloco_ctx* c, const autoloco_sequences* s, const
             hipError_t e = hipSuccess;
             if (a.logits.rows > 0) e = launch_row_logp(bf16, a, c->stream);
             // The gradient's kernel sees to the pairs itself, each row adding its pair's
-            // rows up again, where those are few or small beside the row (30 rows of
-            // 32,000: 13.1 us against 15.4; 1,347 of 1,000: 13.4 against 15.9; 19,456 of
-            // 32,000, 1,216 a pair: 540 against 556; but 9,678 of 1,000, 605 a pair: 36 against 31).
+            // rows up again, where even a pair that has all the rows costs no more so than
+            // a kernel of its own.  How long a pair is only the device knows; one long pair
+            // among short ones makes it the square of its rows.  Eight pairs of bf16 rows,
+            // all alike and (one with nearly all rows), in the gradient's kernel against
+            // apart: 4,096 of 1,000 15.7 us (21.1) against 17.2 (20.2), 8,000 of them 21.7
+            // (32.4) against 21.5 (28.0); 2,048 of 4,096 18.0 (18.6) against 18.4 (19.9),
+            // 4,096 of them 27.8 (31.6) against 26.0 (29.0); 8,000 of 32,000 252 (270)
+            // against 257 (263); of sixteen pairs with 19,456 of 32,000 628 (718) against
+            // 630 (652), of 64 with 32,000 of 4,096 164 (401) against 143 (170).
             const bool writes = grads && a.logits.rows > 0 && a.logits.cols > 0;
             const int64_t row_bytes = a.logits.cols * element_size(s->logits.dtype);
-            const bool together = writes && a.sequences > 0 &&
-                                  (a.logits.rows <= 2048 || a.logits.rows <= a.sequences / 2 * (row_bytes / 16));
+            const int64_t most = row_bytes <= 4096 ? 4096 : std::max<int64_t>(2048, row_bytes / 8);
+            const bool together = writes && a.sequences > 0 && a.logits.rows <= most;
             if (e == hipSuccess && a.sequences > 0 && !together) e = launch_pairs(a, pa, c->stream);
             if (e == hipSuccess && writes) e = launch_logit_grad(bf16, together, a, pa, out_view(p->grads), c->stream);
             return e;

@@ -13,11 +13,12 @@ namespace {
 // exp and 512 for the gradient (19,456 rows of 32,000 bf16: a call 511 us with 256 in
 // both, 502 so); 256 up to rows of 16 KB; a wave up to 4 KB, where a thread of more has
 // no whole vector.
-int threads_of(int64_t rows, int64_t row_bytes, int most) {
+int threads_of(bool few_rows, int64_t row_bytes, int most) {
     if (row_bytes <= 4096) return 64;
     if (row_bytes <= 16384) return 256;
-    return rows <= 512 ? 1024 : most;
+    return few_rows ? 1024 : most;
 }
+constexpr int64_t kFewRows = 512;
 
 // f(integral_constant) of the threads.
 template <typename F>
@@ -44,7 +45,7 @@ hipError_t in_slices(int64_t rows, Launch launch) {
 
 template <bool BF16>
 hipError_t row_logp(const SequenceArgs& a, hipStream_t s) {
-    const int threads = threads_of(a.logits.rows, a.logits.cols * (BF16 ? 2 : 4), 256);
+    const int threads = threads_of(a.logits.rows <= kFewRows, a.logits.cols * (BF16 ? 2 : 4), 256);
     return in_slices(a.logits.rows, [&](int64_t first, dim3 grid) {
         with_threads(threads, [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
@@ -55,13 +56,14 @@ hipError_t row_logp(const SequenceArgs& a, hipStream_t s) {
 
 template <bool BF16>
 hipError_t logit_grad(bool pairs, const SequenceArgs& a, const PreferenceArgs& p, const MatrixOut& g, hipStream_t s) {
-    const int threads = threads_of(a.logits.rows, a.logits.cols * (BF16 ? 2 : 4), 512);
+    // few rows have their pairs in the same kernel, but where there are no pairs: then all is zero
+    const int threads = threads_of(pairs && a.logits.rows <= kFewRows, a.logits.cols * (BF16 ? 2 : 4), 512);
     return in_slices(a.logits.rows + (pairs ? a.sequences / 2 : 0), [&](int64_t first, dim3 grid) {
         with_threads(threads, [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
             if (pairs)
                 hipLaunchKernelGGL((logit_grad_kernel<BF16, NT, true>), grid, dim3(NT), 0, s, a, p, g, first);
-            else
+            else if constexpr (NT != 1024)
                 hipLaunchKernelGGL((logit_grad_kernel<BF16, NT, false>), grid, dim3(NT), 0, s, a, p, g, first);
         });
     });
