@@ -118,10 +118,11 @@ __global__ void __launch_bounds__(kBlock) grad_norm_kernel(GradNormArgs a) {
 }
 
 // Clipping coefficient from a squared norm; NaN stays NaN.
-__device__ __forceinline__ float clip_coef(double norm_sq, double max_norm) {
+__device__ __forceinline__ double clip_ratio(double norm_sq, double max_norm) {
     const double c = max_norm / (sqrt(norm_sq) + 1e-6);
-    return (float)(c > 1.0 ? 1.0 : c);
+    return c > 1.0 ? 1.0 : c;
 }
+__device__ __forceinline__ float clip_coef(double norm_sq, double max_norm) { return (float)clip_ratio(norm_sq, max_norm); }
 
 __device__ __forceinline__ void adamw_one(const AdamWArgs& a, float coef, float& p, float& m, float& v, float g) {
     g *= coef;

@@ -118,10 +118,25 @@ __device__ __forceinline__ double chunk_squares(const GradChunk& c) {
     if (threadIdx.x == 0) a.partials[(int64_t)k * gridDim.x + blockIdx.x] = part;
 }
 
+// A coefficient as two factors, applied one after the other: the first is 1, or a power of
+// two that takes half the exponent of a coefficient which fp32 might not hold, so that
+// huge gradients clipped to a tiny norm do not become 0.
+struct ClipFactors {
+    float first = 1.0f, second = 1.0f;
+    __device__ __forceinline__ explicit ClipFactors(double c) : second((float)c) {
+        if (c < 0x1p-60 && c > 0.0) {
+            const int half = -ilogb(c) / 2;
+            first = (float)ldexp(1.0, -half);
+            second = (float)ldexp(c, half);
+        }
+    }
+    __device__ __forceinline__ float operator()(float g) const { return second * (first * g); }
+};
+
 // Four elements a vector, so that neighbouring lanes write neighbouring 16 bytes.
 // Nothing is kept in the caches: the gradients pass here for the last time.
 template <bool BF16, bool PACK>
-__device__ __forceinline__ void chunk_scale(const GradChunk& c, float coef) {
+__device__ __forceinline__ void chunk_scale(const GradChunk& c, const ClipFactors& clip) {
     constexpr int E = BF16 ? 2 : 4, D = PACK ? 4 : E;   // bytes of an element read, written
     void* to = PACK ? static_cast<void*>(c.packed) : c.grad;
     over_chunk<4>(
@@ -145,9 +160,9 @@ __device__ __forceinline__ void chunk_scale(const GradChunk& c, float coef) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if constexpr (BF16)
-                        v[j] = coef * (j % 2 == 0 ? bf16_lo(w[u][j / 2]) : bf16_hi(w[u][j / 2]));
+                        v[j] = clip(j % 2 == 0 ? bf16_lo(w[u][j / 2]) : bf16_hi(w[u][j / 2]));
                     else
-                        v[j] = coef * __uint_as_float(w[u][j]);
+                        v[j] = clip(__uint_as_float(w[u][j]));
                 }
                 Out x;
                 if constexpr (D == 2) {
@@ -160,7 +175,7 @@ __device__ __forceinline__ void chunk_scale(const GradChunk& c, float coef) {
                 if (decltype(whole)::value || i + u * kBlock < vectors) __builtin_nontemporal_store(x, o + u * kBlock);
             }
         },
-        [&](int j) { store_one<D == 2>(to, j, coef * load_one<BF16>(c.grad, j)); });
+        [&](int j) { store_one<D == 2>(to, j, clip(load_one<BF16>(c.grad, j))); });
 }
 
 [[maybe_unused]] static __global__ void __launch_bounds__(kBlock) tensor_clip_kernel(ClipArgs a) {
@@ -183,22 +198,22 @@ __device__ __forceinline__ void chunk_scale(const GradChunk& c, float coef) {
         }
     }
     __syncthreads();
-    const float coef = a.max_norm > 0.0 ? clip_coef(total, a.max_norm) : 1.0f;
+    const ClipFactors clip(a.max_norm > 0.0 ? clip_ratio(total, a.max_norm) : 1.0);
     if (i < begin) return;
-    if (c.packed == nullptr && coef == 1.0f) return;   // nothing to change in place
+    if (c.packed == nullptr && clip.second == 1.0f && clip.first == 1.0f) return;   // nothing to change in place
     for (;;) {
         i -= gridDim.x;
         const GradChunk next = a.chunks[i >= begin ? i : begin];
         if (c.packed != nullptr) {
             if (c.bf16)
-                chunk_scale<true, true>(c, coef);
+                chunk_scale<true, true>(c, clip);
             else
-                chunk_scale<false, true>(c, coef);
+                chunk_scale<false, true>(c, clip);
         } else {
             if (c.bf16)
-                chunk_scale<true, false>(c, coef);
+                chunk_scale<true, false>(c, clip);
             else
-                chunk_scale<false, false>(c, coef);
+                chunk_scale<false, false>(c, clip);
         }
         if (i < begin) break;
         c = next;
