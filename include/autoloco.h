@@ -604,7 +604,10 @@ typedef struct {
 /* A list of gradient tensors of `workers` (1..AUTOLOCO_MAX_K) workers, laid out once
  * for the steps to come: the table of their places is copied to the device, the
  * tensors stay the caller's and have to stay where they are until the list is
- * destroyed.  All have a packed place or none.  0 <= count <= 2^20.
+ * destroyed.  The list goes by their places: gradients that a program frees and
+ * allocates again between steps need a new list (its making takes the host about 1 to 3 us
+ * a tensor; keep the tensors and fill them anew where that counts).  All have a packed place
+ * or none.  0 <= count <= 2^20.
  * Errors: E_INVALID, E_ALIGN, E_ALIAS (two tensors overlap), E_DEVICE, E_NOMEM. */
 typedef struct autoloco_grads autoloco_grads;
 int autoloco_grads_create(autoloco_ctx* ctx, const autoloco_grad* tensors, int64_t count, int32_t workers,
@@ -614,7 +617,7 @@ void autoloco_grads_destroy(autoloco_grads* list);
 /* Each worker's gradient norm over all its tensors, ||g||, and c = min(1, max_norm
  * / (||g|| + 1e-6)) as in autoloco_inner_adamw (max_norm = 0: c = 1): packed (or
  * grad) becomes c g.  Squares are summed in fp64 in a fixed order.  norms: [workers]
- * fp32 in device memory, or NULL.  With out the call blocks until the norms are on
+ * fp32 in device memory, apart from all of the list's tensors, or NULL.  With out the call blocks until the norms are on
  * the host; without, it is asynchronous.  A non-finite gradient propagates
  * (finite = 0).  Feed the packed gradients to autoloco_inner_adamw with
  * max_grad_norm = 0.

@@ -805,7 +805,8 @@ def autoloco_preference_loss(ctx: Context, logits, labels, offsets, ref_logps, l
 
 
 class GradList:
-    """An autoloco_grads: the workers' gradient tensors, laid out once.  Holds them."""
+    """An autoloco_grads: the workers' gradient tensors, laid out once.  Holds them: a program that lets its gradients
+    go between steps (zero_grad's set_to_none) has to keep them or make a new list, or the old ones are clipped."""
 
     def __init__(self, handle, workers: int, tensors):
         self.handle, self.workers, self.tensors = handle, workers, tensors

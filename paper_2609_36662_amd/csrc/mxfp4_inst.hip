@@ -93,12 +93,17 @@ hipError_t matmul(const Mx4& a, const Mx4& b, const MatrixOut& out, hipStream_t 
     }
 }
 
-// Rows of the weight a workgroup takes: 16, 32 or 48, the fewest that leave no more
-// workgroups than the chip's 256 compute units, so that none waits for a second one
-// (13 x 4,096 x 11,008 rows of weight, bf16: 15.8, 15.1 and 9.6 us), with sixteen waves
+// Rows of the weight a workgroup takes: 16, 32 or, from 8,193 rows on, 48, the fewest that
+// leave no more workgroups than the chip's 256 compute units, so that none waits for a second
+// one (13 x 4,096 x 11,008 rows of weight, bf16: 15.8, 15.1 and 9.6 us), with sixteen waves
 // where there are few rows to share the columns out over (16 x 11,008 x 4,096 rows: 13.1
 // us against 17.0 with eight), eight otherwise.  Each of x's blocks is quantised once a
-// workgroup.
+// workgroup.  From 12,289 rows on there are more workgroups than units (1 and 13 rows of x,
+// a call: 2,048 x 32,000 10.9 and 13.6 us, 768 x 50,257 9.7 and 12.9).
+// At 17 rows x's form and the tiles take over.  Calls of 16 and 17 rows: 4,096 x 11,008 10.8
+// and 13.8 us, 11,008 x 4,096 13.5 and 25.9, 2,048 x 5,632 8.3 and 11.8; where the weight's rows
+// are many the tiles would already do at 13 to 16 (2,048 x 32,000 14.1 and 13.2, 768 x
+// 50,257 13.1 and 11.7).
 template <bool BF16, int R, int NW>
 hipError_t tokens_at(const MatrixView& x, const Mx4& w, const MatrixOut& y, hipStream_t s) {
     return in_slices((w.rows + 16 * R - 1) / (16 * R), [&](uint32_t first, dim3 grid) {

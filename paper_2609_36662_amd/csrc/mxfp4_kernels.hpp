@@ -330,10 +330,12 @@ __global__ void __launch_bounds__(kBlock) mx_cols_kernel(MatrixView x, Mx4 q, Mx
 // -------------------------------------------------------------- dequantise --
 // A lane writes 16 bytes of each of two neighbouring groups, so that neighbouring lanes
 // write neighbouring ones; a workgroup 16 rows (bf16) or 8, nt workgroups across.  Bound by
-// writing (50,257 x 768 fp32 34 us, 5.1 TB/s; with 32 bytes a lane and values put together
-// from bits 47).  Stores past the caches take 27 us, but whoever reads the values next
-// pays for it: 8,192 x 4,096 fp32 with its 4-bit form taken again 50 and 53 us, multiplied in
-// place 76 against 71; 4,096 x 4,096 26.8 against 25.7 and 35.4 against 33.5.
+// writing: 50,257 x 768 fp32 34 us (5.1 TB/s) one call after another (with 32 bytes a lane and
+// values put together from bits 47).  After another kernel it ends sooner and leaves the
+// caches full: in turn with mx_rows_kernel of that size 27 us, and that one 42 instead of
+// its 32, 70 us for both.  Stores past the caches take 27 us in any case, but whoever reads the
+// values next pays for it: 8,192 x 4,096 fp32 with its 4-bit form taken again 50 and 53 us,
+// multiplied in place 76 against 71; 4,096 x 4,096 26.8 against 25.7 and 35.4 against 33.5.
 template <bool BF16>
 constexpr int kValueRows = BF16 ? 16 : 8;
 template <bool BF16>

@@ -9,11 +9,13 @@
 // different banks.  Operands of later columns are read from LDS while the present ones
 // are multiplied.
 //
-// Bound by power at large sizes: the first kernel of this shape took 267 us (4.1 PFLOP/s)
-// for 8,192 x 8,192 x 8,192 with random codes and 185 us (5.9) with zeros, at the same
-// instructions.  Now 253 us (4.3 PFLOP/s with random codes; a bf16 product of that size by
-// the vendor's library 0.79 ms).  Beyond that the fixed cost of a tile counts (9 us at 256 x
-// 256: filling the stages, the result's way out).
+// 8,192 x 8,192 x 8,192 takes 257 us (4.3 PFLOP/s; a bf16 product of that size by the
+// vendor's library 0.79 ms) with random codes and 203 with zeros, 4,096 x 11,008 x 4,096 105
+// and 92 (each with its counters; in a loop of calls 247 and 195, 96 and 85).  The difference is
+// the clock, which power brings down (2.4 GHz with zeros, 1.90 and 2.10 with random
+// codes).  The matrix cores are busy 54 % and 40 % of the cycles with either: the rest is a
+// loop that waits and the fixed cost of a tile (9 us at 256 x 256: filling the stages, the
+// result's way out).
 #pragma once
 
 #include <hip/hip_runtime.h>

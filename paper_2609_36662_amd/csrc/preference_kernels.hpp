@@ -10,10 +10,10 @@
 //
 // Each row's lse from one reading (a running maximum and sum), each pair's loss and
 // weights in fp64, each row's gradient; the middle one inside the last where that costs
-// less than a launch.  The rows' kernels are bound by HBM; exponentials are taken in base
+// no more than a kernel of its own.  The rows' kernels are bound by HBM; exponentials are taken in base
 // 2.  A row whose label is masked, or that is of no sequence, is not read.  (16 pairs of
-// up to 1,024 tokens, vocabulary 32,000, bf16, 40 % of them prompt: 0.50 ms, 2.98 GB at
-// 5.9 TB/s.  Of these 0.87 GB are the second reading of the logits, which the weights
+// up to 1,024 tokens, vocabulary 32,000, bf16, 40 % of them prompt: 0.49 ms, 2.98 GB at
+// 6.0 TB/s.  Of these 0.87 GB are the second reading of the logits, which the weights
 // stand between; pairs that the Infinity Cache holds go only 10 % faster.)
 #pragma once
 
