@@ -643,7 +643,8 @@ __device__ __forceinline__ void direct_tile(const Terms& terms, uint32_t ti, uin
     constexpr int D = TM * TN == 16 ? 1 : 2;   // phases that operands are read ahead
     Frags f[2 * D];
     auto reading = [&](uint32_t stage, auto phase_of) {
-        return [&, stage](auto j) { read(f[decltype(phase_of)::value % (2 * D)], stage, phase_of, j); };
+        typedef decltype(phase_of) Part;   // the lambda outlives the parameter, whose type is all it needs
+        return [&, stage](auto j) { read(f[Part::value % (2 * D)], stage, Part{}, j); };
     };
     auto run = [&](auto phase_of, auto more, auto x, auto x_op) {
         constexpr int s = decltype(phase_of)::value, to = (s + D) % 4;
