@@ -509,7 +509,7 @@ int autoloco_inner_muon(autoloco_ctx* c, autoloco_muon* l, const autoloco_muon_c
                 MuonStep s{};
                 s.matrices = static_cast<const MuonMatrix*>(l->matrices.p);
                 s.momentum = static_cast<float>(k->momentum);
-                s.eps = static_cast<float>(k->eps);
+                s.eps = k->eps > 0.0 ? std::max(k->eps, kMuonLeastEps) : 0.0;
                 s.lr = static_cast<float>(k->lr);
                 s.decay = static_cast<float>(1.0 - k->lr * k->weight_decay);
                 s.nesterov = k->nesterov != 0;

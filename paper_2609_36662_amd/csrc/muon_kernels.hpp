@@ -34,6 +34,9 @@ namespace autoloco {
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kScaleA = 2048.f;
 constexpr int kMuonParts = 256;    // partial sums of a matrix's norm at most
+// A smaller eps counts as this one: beside the norm of anything but zeros (2^-149 at least) neither
+// does, and of zeros the scale over it is finite.
+constexpr double kMuonLeastEps = 1e-300;
 
 // What a step needs of one matrix, in device memory.
 struct MuonMatrix {
@@ -70,7 +73,8 @@ struct MuonTile {
 struct MuonStep {
     const MuonMatrix* matrices;
     const MuonTile* tiles;
-    float momentum, eps, decay, lr;   // decay: 1 - lr weight_decay
+    double eps;                       // above zero: at least kMuonLeastEps
+    float momentum, decay, lr;        // decay: 1 - lr weight_decay
     int32_t nesterov, spectral, from; // from: which of hi a product reads
 };
 
@@ -169,7 +173,7 @@ static __global__ void __launch_bounds__(256) muon_start_kernel(MuonStep s) {
     }
     __syncthreads();
     // in fp64: norms beyond the range of fp32's reciprocals are fine
-    const double factor = (double)x.scale / (sqrt(part[0] + part[1] + part[2] + part[3]) + (double)s.eps);
+    const double factor = (double)x.scale / (sqrt(part[0] + part[1] + part[2] + part[3]) + s.eps);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
