@@ -172,8 +172,10 @@ static __global__ void __launch_bounds__(256) muon_start_kernel(MuonStep s) {
         }
     }
     __syncthreads();
-    // in fp64: norms beyond the range of fp32's reciprocals are fine
-    const double factor = (double)x.scale / (sqrt(part[0] + part[1] + part[2] + part[3]) + s.eps);
+    // in fp64: norms beyond the range of fp32's reciprocals are fine.  An infinite one leaves no
+    // direction: all of X is NaN, not only what was infinite.
+    const double norm = sqrt(part[0] + part[1] + part[2] + part[3]);
+    const double factor = __builtin_isinf(norm) ? (double)__builtin_nanf("") : (double)x.scale / (norm + s.eps);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
