@@ -1,6 +1,7 @@
 // Entry points of the feed-forward half of a block: the norms around it, the gated block,
 // the orthogonalised step of its matrices.
 #include <algorithm>
+#include <limits>
 #include <memory>
 
 #include "gated_ff_kernels.hpp"
@@ -14,10 +15,18 @@ namespace {
 
 constexpr int64_t kMaxFf = int64_t(1) << 24;       // rows and widths of a block
 constexpr int64_t kMaxMuon = int64_t(1) << 16;     // rows and columns of a matrix
+constexpr double kMuonMaxScale = 256.0;            // s at most: the root of rows over columns
 // Bytes of X, A and B of a batch, unless one matrix takes more: the more tiles a launch has, the
 // less its last round counts (a layer of 4,096 x 11,008 in one batch
 // 16.3 ms, in two of at most 1 GiB 17.8).
 constexpr int64_t kMuonScratch = int64_t(4) << 30;
+
+// The least eps of a row's mean square that the kernels' fp32 holds to half a rounding step: below, it
+// would be rounded coarsely, or to zero, which makes a row of zeros NaN.
+constexpr double kLeastEps = 0x1p-126;
+
+// Whether a scalar is finite as the fp32 value that the kernels use.
+bool fits(double v) { return std::fabs(v) <= std::numeric_limits<float>::max(); }
 
 // A matrix of rows x cols and dtype (-1: either).
 int check_shape(autoloco_ctx* c, const autoloco_matrix& m, const char* name, int64_t rows, int64_t cols, int32_t dtype, bool written) {
@@ -70,8 +79,9 @@ int check_stream(autoloco_ctx* c, const autoloco_residual& r, const autoloco_mat
     int st = check_matrix(c, stream, name, false);
     if (st != AUTOLOCO_OK) return st;
     if (stream.cols > kMaxNormCols) return fail(c, AUTOLOCO_E_INVALID, "more than 2^15 columns");
-    if (!std::isfinite(r.scale) || !(std::isfinite(r.eps) && r.eps >= 0.0))
-        return fail(c, AUTOLOCO_E_INVALID, "scale must be finite, eps finite and >= 0");
+    if (!fits(r.scale) || !(fits(r.eps) && r.eps >= 0.0))
+        return fail(c, AUTOLOCO_E_INVALID, "scale must be finite, eps finite and >= 0 (in fp32)");
+    if (r.eps > 0.0 && r.eps < kLeastEps) return fail(c, AUTOLOCO_E_INVALID, "eps between 0 and 2^-126");
     if (given(r.z)) {
         if ((st = check_shape(c, r.z, "z", stream.rows, stream.cols, stream.dtype, false)) != AUTOLOCO_OK) return st;
         if (given(r.gate) && (st = check_shape(c, r.gate, "gate", stream.rows, stream.cols, stream.dtype, false)) != AUTOLOCO_OK)
@@ -501,6 +511,8 @@ int autoloco_inner_muon(autoloco_ctx* c, autoloco_muon* l, const autoloco_muon_c
         if (!(std::isfinite(k->lr) && k->lr >= 0.0 && std::isfinite(k->weight_decay) && k->weight_decay >= 0.0 && std::isfinite(k->eps) &&
               k->eps >= 0.0))
             return fail(c, AUTOLOCO_E_INVALID, "lr, weight_decay and eps must be finite and >= 0");
+        if (!fits(k->lr * kMuonMaxScale) || !fits(k->lr * k->weight_decay))
+            return fail(c, AUTOLOCO_E_INVALID, "lr, or lr times weight_decay, leaves fp32");
         if (!(k->momentum >= 0.0 && k->momentum < 1.0)) return fail(c, AUTOLOCO_E_INVALID, "momentum outside [0, 1)");
         if (k->iterations < 0 || k->iterations > 16) return fail(c, AUTOLOCO_E_INVALID, "iterations outside 0..16");
         if (k->scale != AUTOLOCO_MUON_RMS && k->scale != AUTOLOCO_MUON_SPECTRAL) return fail(c, AUTOLOCO_E_INVALID, "unknown scale");
