@@ -104,7 +104,7 @@ __device__ __forceinline__ void load_grad(float (&g)[8], const MuonMatrix& x, in
 }
 
 // M <- mu M + G and a part of |U|^2, in fp64, eight neighbours of a row at a time.
-static __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonStep s) {
+[[maybe_unused]] static __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonStep s) {
     __shared__ double part[4];
     const MuonTile t = s.tiles[blockIdx.x];
     const MuonMatrix x = s.matrices[t.matrix];
@@ -147,7 +147,7 @@ static __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonStep s) {
 // X = U / (|U| + eps), scaled, in two parts; zeros up to whole steps of the products.  A
 // workgroup takes 64 x 64 of X, eight neighbours of the tensor's rows a lane; of a tall
 // matrix they are turned in LDS.
-static __global__ void __launch_bounds__(256) muon_start_kernel(MuonStep s) {
+[[maybe_unused]] static __global__ void __launch_bounds__(256) muon_start_kernel(MuonStep s) {
     __shared__ double part[4];
     __shared__ float turn[64][65];
     const MuonTile t = s.tiles[blockIdx.x];
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(256, tile_groups(TM, TN, ST)) muon_product_ker
 }
 
 // W from X where there are no iterations.
-static __global__ void __launch_bounds__(256) muon_apply_kernel(MuonStep s) {
+[[maybe_unused]] static __global__ void __launch_bounds__(256) muon_apply_kernel(MuonStep s) {
     const MuonTile t = s.tiles[blockIdx.x];
     const MuonMatrix& x = s.matrices[t.matrix];
     const int64_t i0 = (int64_t)t.i * 64, j0 = (int64_t)t.j * 64;

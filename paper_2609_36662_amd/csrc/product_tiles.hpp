@@ -602,7 +602,12 @@ __device__ __forceinline__ void direct_tile(const Terms& terms, uint32_t ti, uin
         const uint8_t* tile = lds + stage + (a ? 0 : kTile);
         constexpr int B = a ? BA : BB;
         const uint32_t row = ((a ? wm * TM : wn * TN) + t) * 32;
-        u32x4& to = a ? f.a[t] : f.b[t];
+        u32x4& to = [&]() -> u32x4& {
+            if constexpr (a)
+                return f.a[t];
+            else
+                return f.b[t];
+        }();
         if constexpr (tr) {
             const u32x2r v = turned_half<B>(tile, row, s, lane, jj & 1);
             to[2 * (jj & 1)] = v[0];
