@@ -23,10 +23,7 @@ MatrixView read(const MatrixOut& m) { return {m.data, m.rows, m.cols, m.stride};
 
 template <bool AT, bool BT, bool PAIR, typename Epi>
 hipError_t product(const Terms& t, int64_t rows, int64_t cols, const Epi& epi, hipStream_t s) {
-    auto grid_of = [&](TileSize size) {
-        const int64_t height = tile_rows(size), width = PAIR ? tile_cols(size) / 2 : tile_cols(size);
-        return Tiles{(uint32_t)((rows + height - 1) / height), (uint32_t)((cols + width - 1) / width)};
-    };
+    auto grid_of = [&](TileSize size) { return grid_of_product(size, rows, cols, PAIR); };
     bool direct = true;
     int64_t k = 0;
     for (int i = 0; i < t.count; ++i) {
@@ -49,18 +46,7 @@ hipError_t product(const Terms& t, int64_t rows, int64_t cols, const Epi& epi, h
             if ((int64_t)g.mt * g.nt < 256) return through_registers(TILE_64, std::integral_constant<int, 1>{});
         return through_registers(TILE_128, std::integral_constant<int, 2>{});
     }
-    TileSize best = TILE_128;
-    double least = 1e300;
-    for (int i = 0; i < TILE_SIZES; ++i) {
-        const TileSize size = (TileSize)i;
-        if (PAIR && size == TILE_64) continue;
-        const Tiles g = grid_of(size);
-        const double us = tile_us(size, (int64_t)g.mt * g.nt, (double)k / 64);
-        if (us < least) {
-            least = us;
-            best = size;
-        }
-    }
+    const TileSize best = tile_of_product(rows, cols, k, PAIR);
     const Tiles g = grid_of(best);
     return with_tile(best, [&](auto tm, auto tn, auto stages) -> hipError_t {
         constexpr int TM = decltype(tm)::value, TN = decltype(tn)::value, ST = decltype(stages)::value;

@@ -480,6 +480,27 @@ inline double tile_us(TileSize size, int64_t tiles, double s) {
 }
 constexpr int64_t tile_rows(TileSize size) { return size == TILE_256 || size == TILE_256_128 ? 256 : size == TILE_64 ? 64 : 128; }
 constexpr int64_t tile_cols(TileSize size) { return size == TILE_256 ? 256 : size == TILE_64 ? 64 : 128; }
+// The tiles of a result.  A pair's take half as many columns of each of its matrices, and 32 at least.
+inline Tiles grid_of_product(TileSize size, int64_t rows, int64_t cols, bool pair) {
+    const int64_t height = tile_rows(size), width = pair ? tile_cols(size) / 2 : tile_cols(size);
+    return Tiles{(uint32_t)((rows + height - 1) / height), (uint32_t)((cols + width - 1) / width)};
+}
+// The size with the least time for rows x cols of k summed elements.
+inline TileSize tile_of_product(int64_t rows, int64_t cols, int64_t k, bool pair) {
+    TileSize best = TILE_128;
+    double least = 1e300;
+    for (int i = 0; i < TILE_SIZES; ++i) {
+        const TileSize size = static_cast<TileSize>(i);
+        if (pair && size == TILE_64) continue;
+        const Tiles g = grid_of_product(size, rows, cols, pair);
+        const double us = tile_us(size, (int64_t)g.mt * g.nt, static_cast<double>(k) / 64);
+        if (us < least) {
+            least = us;
+            best = size;
+        }
+    }
+    return best;
+}
 // f(integral_constants: a wave's 32 rows and 32 columns, stages) of a size.
 template <typename F>
 auto with_tile(TileSize size, F f) {
