@@ -140,7 +140,8 @@ template <int NW, int U, bool PAIR, typename Epi>
 __global__ void __launch_bounds__(NW * 64) tokens_kernel(MatrixView x, Operand w, const uint16_t* w2, uint32_t first, Epi epi) {
     constexpr int R = PAIR ? 2 : 1;
     typedef __bf16 v8 __attribute__((ext_vector_type(8)));
-    __shared__ float part[NW][R * 256];
+    __shared__ __align__(16) float part[NW][R * 256];
+    static_assert(__alignof__(part) >= 16, "stored four at a time");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r = lane & 15, q = lane >> 4;
     const int64_t n0 = ((int64_t)first + blockIdx.x) * 16;

@@ -307,7 +307,8 @@ __global__ void __launch_bounds__(team_threads(W)) residual_grad_kernel(Residual
     }
     if (a.work == nullptr) return;
     // the workgroup's part of each sum, its teams in order
-    __shared__ float join[W == 1 ? 4 * C * 512 : 1];
+    __shared__ __align__(16) float join[W == 1 ? 4 * C * 512 : 1];
+    static_assert(__alignof__(join) >= 16, "stored four at a time");
     auto put = [&](const float (&v)[C][8], int which) {
         float* to = a.work + ((int64_t)which * gridDim.x + blockIdx.x) * cols;
         if constexpr (W == 1) {
