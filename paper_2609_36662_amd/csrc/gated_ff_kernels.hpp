@@ -9,13 +9,16 @@
 // the sums of a product whose epilogue reads g and u and writes dg and du.  dx adds both
 // its terms up in one sum.  h, and of training g and u, dg and du, are rounded to bf16,
 // since they are the next products' operands; everything else is fp32 up to the outputs' rounding.
+// (y and dWd are 0.235 % of their norm off by it, where their own rounding alone is 0.166; dx, dWg
+// and dWu 0.30 %.)
 //
-// Bound by the matrix cores for many rows and by rounds of tiles that are not full.  Measured
-// among other calls: 2,048 rows of 4,096 with 11,008 between, both projections 332 to 357
-// us (1.04 to 1.11 PFLOP/s, cores busy 60 %) and the last product 177 (1.04); 4,096 rows of 2,048 with 5,632
-// between, g, u and h kept 204 to 213 us (0.9), y 93 us (1.02), dh 140 us (0.67; g and u
-// read, dg and du written), dx 180 to 186 us (1.0), each weights' gradient 107 to 110 us (0.87: 176
-// tiles of 256 on 256 units).
+// Bound by the matrix cores for many rows and by rounds of tiles that are not full.  Among
+// other calls (medians; cards and runs lie up to 5 % to either side): 2,048 rows of 4,096 with
+// 11,008 between, both projections 355 us (1.04 PFLOP/s, cores busy 60 %) and the last product 181
+// (1.02); 4,096 rows of 2,048 with 5,632 between, g, u and h kept 204 us (0.93), y 92 us (1.03), dh
+// 136 us (0.69; g and u read, dg and du written), dx 183 us (1.03), each weights' gradient 107 us
+// (0.88: 176 tiles of 256 on 256 units; in a loop over the same operands 89 us, in fp32, whose
+// words are stored one by one, 116).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -132,10 +135,11 @@ __global__ void __launch_bounds__(256, tile_groups(TM, TN, ST)) direct_kernel(Te
 // Up to 16 rows: a workgroup takes 16 columns of the result (PAIR: of both projections),
 // its NW waves the summed axis in turn, joined in LDS in wave order.  A lane takes its
 // column's weight and its row of x straight from memory, 8 elements of each, as the 16x16x32
-// instruction wants them.  Bound by the weights' bytes: 1 row of 2,048 with 5,632 between 14.8
-// and 8.3 us (3.1 and 2.8 TB/s: two short launches), 13 rows of 4,096 with 11,008 between 37.8
-// and 22.2 us (4.8 and 4.1 TB/s).  Whole lines are read at a time; by halves, past the caches, the
-// two calls took 26.6 and 80 us for 21.6 and 68.
+// instruction wants them.  Bound by the weights' way from memory: 13 rows of 4,096 with 11,008
+// between 38 and 22 us (4.7 and 4.1 TB/s).  1 row of 2,048 with 5,632 between 14.6 and 8.5 us (3.2 and
+// 2.7 TB/s): the first launch's waves make four rounds of loads, each waiting for the one before, and
+// the second has 128 workgroups for 256 units.  Whole lines are read at a time; by halves, past the
+// caches, the two calls took 26.6 and 80 us for 21.6 and 68.
 template <int NW, int U, bool PAIR, typename Epi>
 __global__ void __launch_bounds__(NW * 64) tokens_kernel(MatrixView x, Operand w, const uint16_t* w2, uint32_t first, Epi epi) {
     constexpr int R = PAIR ? 2 : 1;
@@ -149,7 +153,7 @@ __global__ void __launch_bounds__(NW * 64) tokens_kernel(MatrixView x, Operand w
     const uint16_t* from[2] = {w.p + wr * w.stride, PAIR ? w2 + wr * w.stride : nullptr};
     const uint16_t* xr = static_cast<const uint16_t*>(x.data) + (r < x.rows ? r : x.rows - 1) * x.stride;
     f32x4 acc[R] = {};
-    // U pieces of 32 on their way at a time, the weights past the caches
+    // U pieces of 32 on their way at a time
     const int64_t whole = x.cols / (NW * U * 32) * (NW * U * 32);
     auto multiply = [&](u32x4 a, u32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, b), __builtin_bit_cast(v8, a), c, 0, 0, 0);

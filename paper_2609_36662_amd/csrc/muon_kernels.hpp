@@ -19,9 +19,10 @@
 // in bf16 2e-2 and 3e-1.)
 //
 // Bound by the matrix cores for large matrices, by the tiles' first loads and epilogues for
-// sums of few steps.  One layer of 4,096 and 11,008 (tiles of 256; us, cores busy): A 786, 60 %;
-// B 523, 50 %; X 1,688, 51 %; the last X with W 2,123, 38 %; M 407 (4.7 TB/s) and U 418.  Two
-// times four layers of 768 and 2,048 (tiles of 128): 99, 22 %; 77, 16 %; 191, 21 %; 286, 14 %.
+// sums of few steps.  One layer of 4,096 and 11,008 (tiles of 256; us, cores busy; cards lie
+// up to 3 % to either side): A 800, 60 %; B 530, 50 %; X 1,730, 51 %; the last X with W 2,170, 38 %; M 406
+// (4.7 TB/s) and U 418.  Two times four layers of 768 and 2,048 (tiles of 128): 100, 22 %; 78, 16 %;
+// 193, 21 %; 290, 14 %.
 #pragma once
 
 #include <hip/hip_runtime.h>

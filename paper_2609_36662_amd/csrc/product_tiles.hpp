@@ -364,7 +364,7 @@ __device__ __forceinline__ void finish_turned(const f32x16 (&acc)[TM][T], uint8_
 // sizes and addresses: the pieces of the next Q steps are on their way while one is multiplied.
 // Bound by the loads' latency and the turn through registers: 4,095 rows of 2,047 with 5,631
 // between take 488 us forward (0.58 PFLOP/s), 482 for dg, du and dx, 643 for the three weights'
-// gradients (0.44); 300 rows of 771 with 1,030 between 27, 11, 16, 19 and three times 7 us.  No
+// gradients (0.44); 300 rows of 771 with 1,030 between some 28, 11, 18, 19 and three times 7 us.  No
 // branch stands between a step's loads: with them the compiler waits for all of a step before the
 // next (134 us for both directions of the last, 86 without).
 template <typename E, bool AT, bool BT, int T, bool PAIR, typename Finish>
@@ -465,7 +465,10 @@ inline bool whole_pieces(const Operand& o, int64_t k, bool across) {
 // 123, 141 and 199; 2,048 x 4,096 x 11,008 216, 157 and 164; 4,096 x 5,632 x 2,048 106, 95, 92,
 // 112 and 145; 2,048 x 2,048 x 5,632 106, 72, 64, 49 and 73; 2,048^3 44, 29, 27, 22 and 29; 1,024 x
 // 2,048 x 2,048 42, -, 24, 19 and 15; 1,024 x 1,024 x 4,096 74, -, 42, 31 and 19.  Operands across
-// take the same within 5 %.
+// take the same within 5 %.  These are products that store one matrix; the rule knows nothing of what
+// an epilogue reads and writes beyond that, and says 97 us for dh of 4,096 x 5,632 x 2,048 (136 measured
+// among other calls), 160 for the projections of that size with g, u and h kept (204), 288 for 2,048 x 11,008
+// x 4,096 with h alone (355).  Whether another tile would suit dh better was not measured.
 enum TileSize { TILE_256, TILE_256_128, TILE_128, TILE_128_DEEP, TILE_64, TILE_SIZES };
 inline double tile_us(TileSize size, int64_t tiles, double s) {
     const int64_t slots = size == TILE_128 || size == TILE_64 ? 512 : 256;

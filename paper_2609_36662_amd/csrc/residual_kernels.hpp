@@ -11,9 +11,9 @@
 // LDS.  In the backward pass a team of waves goes from row to row and keeps its columns' part
 // of dw, dwz and a channel's dgate in registers; the workgroups' parts are added up in fp64, in a
 // fixed order, by a second kernel.
-// Bound by HBM: 16,384 x 2,048 bf16 among other calls 57 us forward (4.7 TB/s), 85 us backward
-// (4.7 TB/s) and 13 us for the second kernel; a loop over the same rows finds a part of them in
-// the last cache (45, 81 and 7).
+// Bound by HBM: 16,384 x 2,048 bf16 among other calls 56 to 57 us forward (4.7 TB/s), 84 to 88 us
+// backward (4.7 TB/s) and 13 us for the second kernel (96 workgroups that each add up 128 KB); a
+// loop over the same rows finds a part of them in the last cache (45, 81 and 7).
 #pragma once
 
 #include <hip/hip_runtime.h>
